@@ -341,6 +341,106 @@ MLPMOE_API int mlpmoe_forward_routed_f32_ws(const float *x, const float *W_gate,
                                             size_t workspace_bytes, void *stream);
 
 /*
+ * mlpmoe_route_topk -- the router of a routed layer: which branches each token takes.
+ *
+ * For token t and the branches b with active_mask[b] != 0, x = logits[t * ld + b] widened to float:
+ *     probs[t, b] = exp(x_b - max x) / sum exp(x - max x), 0 for the other branches;
+ *     route[t, b] = 1 for the k branches that come first in the order "larger logit, then lower index", else 0.
+ * A logit of minus infinity bars its branch: probability 0, never taken, so a token may take fewer than k.  A token with
+ * token_mask[t] == 0 (padding) and one whose branches are all barred take nothing, have probabilities of 0 and are not counted.
+ * The route feeds mlpmoe_forward_routed_* and mlpmoe_forward_w4.
+ *     counts[b]   = tokens that take branch b,   counts[B] = N, the tokens counted
+ *     loss        = A * sum_b f_b P_b,  A the number of active branches, f_b = counts[b] / sum_b counts[b],
+ *                   P_b = (1 / N) sum_t probs[t, b]:  1 if the branches are taken and weighted evenly; 0 if nothing is taken
+ * (the balance term of a training loss; the paper names routing as the next step, Sec. 7, and defines no loss).
+ *
+ *   logits       device [T, B], rows ld >= B elements apart, bf16 (elem_bytes 2) or float (4), each on its own alignment
+ *   active_mask  HOST, B bytes or NULL: all branches.  Logits of the other branches are never looked at
+ *   token_mask   device, T bytes or NULL: every token counts
+ *   k            1 <= k <= B
+ *   route        device, T * B bytes
+ *   probs        device float [T, B], or NULL
+ *   counts, loss device int32 [B + 1] and one float, or NULL, each for itself.  Without either the call is one launch and needs no
+ *                workspace
+ * An active logit that is not a number is never taken and makes its token's probabilities, and the loss, not a number; so does
+ * plus infinity, which is taken first.  Arithmetic in float; sums over tokens in float within a block of tokens and in double
+ * over the blocks, in an order that follows from T and B: results are the same bits from run to run.  No output may overlap
+ * an input.  T >= 0 (T == 0: counts and loss are set to zero), T <= 2^24, 1 <= B <= MLPMOE_MAX_BRANCHES.
+ * Workspace as for mlpmoe_forward_bf16: mlpmoe_set_workspace()'s block or the library's own; the _ws form takes the caller's,
+ * 256-byte aligned, of mlpmoe_route_workspace_bytes(T, B) bytes (0 for invalid sizes), scratch.
+ * Errors: NULL, SHAPE, UNSUPPORTED (elem_bytes), ALIGN, WORKSPACE, HIP.
+ */
+MLPMOE_API size_t mlpmoe_route_workspace_bytes(int T, int B);
+MLPMOE_API int mlpmoe_route_topk(const void *logits, int ld, const uint8_t *active_mask, const uint8_t *token_mask, int T,
+                                 int B, int k, int elem_bytes, uint8_t *route, float *probs, int32_t *counts, float *loss,
+                                 void *stream);
+MLPMOE_API int mlpmoe_route_topk_ws(const void *logits, int ld, const uint8_t *active_mask, const uint8_t *token_mask, int T,
+                                    int B, int k, int elem_bytes, uint8_t *route, float *probs, int32_t *counts, float *loss,
+                                    void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * mlpmoe_route_backward -- the gradient with respect to the router's logits.
+ *     g[t, b]       = dprobs[t, b] + dloss * A * f_b / N          (f_b and N as above, held fixed: counts have no gradient)
+ *     dlogits[t, b] = probs[t, b] * (g[t, b] - sum_c probs[t, c] g[t, c])
+ * A probability of 0 has no part in the sum and a gradient of 0, whatever dprobs holds there: barred and inactive branches,
+ * padding.
+ *
+ *   probs    device float [T, B], as mlpmoe_route_topk left them
+ *   counts   device int32 [B + 1], as mlpmoe_route_topk left them; NULL is fine without dloss
+ *   dprobs   device float [T, B], or NULL: nothing but the loss depends on the probabilities
+ *   dloss    device, one float, or NULL: the loss is not used
+ *   active_mask  HOST, B bytes or NULL, as given to mlpmoe_route_topk
+ *   dlogits  device [T, B], rows B elements apart, bf16 (elem_bytes 2) or float (4); must not overlap an input
+ * One launch, no workspace.  Errors: NULL, SHAPE, UNSUPPORTED (elem_bytes), ALIGN, HIP.
+ */
+MLPMOE_API int mlpmoe_route_backward(const float *probs, const int32_t *counts, const float *dprobs, const float *dloss,
+                                     const uint8_t *active_mask, int T, int B, int elem_bytes, void *dlogits, void *stream);
+
+/*
+ * 4-bit weights: the public Microscaling format MXFP4.  A matrix [rows, cols], cols a multiple of 32, is
+ *     codes  [rows, cols / 2] bytes: element 2i of a row in the low four bits of byte i, element 2i + 1 in the high four; sign and
+ *            magnitude, the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ *     scales [rows, cols / 32] bytes: elements 32i .. 32i + 31 of a row are multiplied by 2^(s - 127); s = 255: not a number
+ * 4.25 bits a weight; every value is exact in bf16 (2^128 and more, at s = 253 and 254: infinity).  device, 16-byte aligned.
+ *
+ * mlpmoe_w4_quantize     of W, bf16 (elem_bytes 2) or float (4): s = 127 + floor(log2(largest magnitude of the block)) - 2, at least 1;
+ *                        elements rounded to nearest, halfway to the even code, magnitudes above 6 to 6.  A block with an infinity or a
+ *                        not-a-number gets s = 255
+ * mlpmoe_w4_dequantize   the values, in bf16 or float
+ * Buffers must not overlap.  Errors: SHAPE, UNSUPPORTED (elem_bytes, cols), NULL, ALIGN, HIP.
+ */
+MLPMOE_API int mlpmoe_w4_quantize(const void *W, int rows, int cols, int elem_bytes, uint8_t *codes, uint8_t *scales, void *stream);
+MLPMOE_API int mlpmoe_w4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, int elem_bytes, void *W,
+                                    void *stream);
+
+/*
+ * mlpmoe_forward_w4 / _ws -- the bf16 forward, plain or routed, on 4-bit weights: W_gate and W_up [d_inter, d_model], W_down
+ * [d_model, d_inter] as codes and scales each.  x, branch_offsets, alpha, active_mask, T, d_model, d_inter and B as for
+ * mlpmoe_forward_bf16; route as for mlpmoe_forward_routed_bf16, or NULL: every token takes every active branch.  d_model and
+ * d_inter are multiples of 32 (MLPMOE_ERR_UNSUPPORTED otherwise; mlpmoe_slice_rows makes row counts of compacted layers so),
+ * branch boundaries may lie anywhere.
+ *
+ * Arithmetic: that of mlpmoe_forward_bf16 on the dequantised weights, h rounded once to bf16, sums in float; out is float
+ * (out_bytes 4) or the sums rounded once to bf16 (2), [T, d_model].  It may overlap x.  Results are the same bits from run to
+ * run.  An inactive branch, and one that no token takes, contributes nothing: no value of its weights reaches out, unless a block of
+ * W_down that it shares with a neighbour has the scale 255.
+ *
+ * Workspace as for mlpmoe_forward_bf16; mlpmoe_w4_workspace_bytes() bytes (0 for invalid sizes) for the _ws form.
+ * Errors: those of mlpmoe_forward_bf16, and UNSUPPORTED; T above 1048560 is MLPMOE_ERR_SHAPE.
+ */
+MLPMOE_API size_t mlpmoe_w4_workspace_bytes(int T, int d_model, int d_inter, int B);
+MLPMOE_API int mlpmoe_forward_w4(const void *x, const uint8_t *gate_codes, const uint8_t *gate_scales, const uint8_t *up_codes,
+                                 const uint8_t *up_scales, const uint8_t *down_codes, const uint8_t *down_scales,
+                                 const int32_t *branch_offsets, const float *alpha, const uint8_t *active_mask,
+                                 const uint8_t *route, int T, int d_model, int d_inter, int B, int out_bytes, void *out,
+                                 void *stream);
+MLPMOE_API int mlpmoe_forward_w4_ws(const void *x, const uint8_t *gate_codes, const uint8_t *gate_scales,
+                                    const uint8_t *up_codes, const uint8_t *up_scales, const uint8_t *down_codes,
+                                    const uint8_t *down_scales, const int32_t *branch_offsets, const float *alpha,
+                                    const uint8_t *active_mask, const uint8_t *route, int T, int d_model, int d_inter, int B,
+                                    int out_bytes, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * mlpmoe_fade -- Fractal Fade weight preparation (Sec. 3.2), in place, on the device.
  *
  * For every branch b with sparsity[b] > 0, and separately for the branch's rows of W_gate and of
@@ -416,7 +516,13 @@ enum {
     MLPMOE_KERNEL_GATE_UP_GENERIC = 6,
     MLPMOE_KERNEL_DOWN_GENERIC = 7,
     MLPMOE_KERNEL_FILL_ZERO = 8,
-    MLPMOE_KERNEL_ROUTE_TILES = 9
+    MLPMOE_KERNEL_ROUTE_TILES = 9,
+    MLPMOE_KERNEL_ROUTE_TOPK = 10,
+    MLPMOE_KERNEL_ROUTE_FINISH = 11,
+    MLPMOE_KERNEL_ROUTE_BACKWARD = 12,
+    MLPMOE_KERNEL_W4_GATE_UP = 13,
+    MLPMOE_KERNEL_W4_DOWN = 14,
+    MLPMOE_KERNEL_W4_CONVERT = 15
 };
 MLPMOE_API int mlpmoe_profile_enable(int capacity);
 MLPMOE_API int mlpmoe_profile_collect(int *ids, float *ms, int capacity);

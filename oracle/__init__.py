@@ -9,3 +9,4 @@ from .forward import (build_oracle, dense_swiglu, mlpmoe_forward, mlpmoe_forward
 from .fade import fade_block, fade_neurons, fractal_fade, linear_quantile, neuron_scores  # noqa: F401
 from .slicing import (compact_layer, compensated_alpha, fade_sparsity, slice_plan,  # noqa: F401
                       split_sizes)
+from . import route, w4  # noqa: F401

@@ -30,7 +30,9 @@ EXPORTS = ["mlpmoe_status_string", "mlpmoe_last_error_detail", "mlpmoe_slice", "
            "mlpmoe_plan_destroy", "mlpmoe_forward_routed_bf16", "mlpmoe_forward_routed_bf16_ws",
            "mlpmoe_forward_bf16_out_bf16", "mlpmoe_forward_bf16_out_bf16_ws",
            "mlpmoe_forward_routed_f32", "mlpmoe_forward_routed_f32_ws", "mlpmoe_set_workspace", "mlpmoe_hidden_ld",
-           "mlpmoe_forward_bf16_noalloc"]
+           "mlpmoe_forward_bf16_noalloc", "mlpmoe_route_workspace_bytes", "mlpmoe_route_topk", "mlpmoe_route_topk_ws",
+           "mlpmoe_route_backward", "mlpmoe_w4_quantize", "mlpmoe_w4_dequantize", "mlpmoe_w4_workspace_bytes",
+           "mlpmoe_forward_w4", "mlpmoe_forward_w4_ws"]
 
 
 class MlpMoeError(RuntimeError):
@@ -99,6 +101,26 @@ def _load() -> ctypes.CDLL:
     lib.mlpmoe_forward_bf16_out_bf16_ws.restype = i
     lib.mlpmoe_forward_f32_ws.argtypes = [vp, vp, vp, vp, ip, fp, bp, i, i, i, i, vp, vp, sz, vp]
     lib.mlpmoe_forward_f32_ws.restype = i
+    topk = [vp, i, bp, vp, i, i, i, i, vp, vp, vp, vp]
+    lib.mlpmoe_route_workspace_bytes.argtypes = [i, i]
+    lib.mlpmoe_route_workspace_bytes.restype = sz
+    lib.mlpmoe_route_topk.argtypes = topk + [vp]
+    lib.mlpmoe_route_topk.restype = i
+    lib.mlpmoe_route_topk_ws.argtypes = topk + [vp, sz, vp]
+    lib.mlpmoe_route_topk_ws.restype = i
+    lib.mlpmoe_route_backward.argtypes = [vp, vp, vp, vp, bp, i, i, i, vp, vp]
+    lib.mlpmoe_route_backward.restype = i
+    lib.mlpmoe_w4_quantize.argtypes = [vp, i, i, i, vp, vp, vp]
+    lib.mlpmoe_w4_quantize.restype = i
+    lib.mlpmoe_w4_dequantize.argtypes = [vp, vp, i, i, i, vp, vp]
+    lib.mlpmoe_w4_dequantize.restype = i
+    lib.mlpmoe_w4_workspace_bytes.argtypes = [i, i, i, i]
+    lib.mlpmoe_w4_workspace_bytes.restype = sz
+    w4 = [vp] * 7 + [ip, fp, bp, vp, i, i, i, i, i, vp]
+    lib.mlpmoe_forward_w4.argtypes = w4 + [vp]
+    lib.mlpmoe_forward_w4.restype = i
+    lib.mlpmoe_forward_w4_ws.argtypes = w4 + [vp, sz, vp]
+    lib.mlpmoe_forward_w4_ws.restype = i
     lib.mlpmoe_release.argtypes = []
     lib.mlpmoe_release.restype = i
     lib.mlpmoe_set_workspace.argtypes = [vp, sz]
@@ -378,6 +400,166 @@ def _forward_routed(name, x, W_gate, W_up, W_down, branch_offsets, alpha, active
     return out
 
 
+# --------------------------------------------------------------------------- the router
+def _here(*tensors):
+    """The tensors of a call lie on the current device, whose stream it is launched on."""
+    dev = _current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise ValueError("expected GPU tensors on the current device")
+
+
+def _bytes_mask(mask, n, what):
+    if mask is None:
+        return None
+    m = _host(mask, np.uint8)
+    if m.shape != (n,):
+        raise ValueError("%s needs %d entries" % (what, n))
+    return m.tobytes()
+
+
+def _out(t, shape, dtype, device, what):
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of %s" % (what, list(shape), dtype))
+    return t
+
+
+def _elem(dtype, what):
+    if dtype == torch.bfloat16:
+        return 2
+    if dtype == torch.float32:
+        return 4
+    raise ValueError("%s must be bfloat16 or float32" % what)
+
+
+def mlpmoe_route_workspace_bytes(T, B) -> int:
+    return int(lib.mlpmoe_route_workspace_bytes(int(T), int(B)))
+
+
+def mlpmoe_route_topk(logits, k, active_mask=None, token_mask=None, route=None, probs=None, want_probs=True,
+                      want_stats=True, workspace=None, stream=None):
+    """The k branches each token takes, from the router's logits [T, B] (bf16 or float32, rows of any stride).
+
+    active_mask: host, B entries; token_mask: GPU, T bytes (uint8 or bool), 0 = padding.  Returns (route [T, B] uint8,
+    probs [T, B] float32 or None, counts [B + 1] int32 or None, loss [1] float32 or None): counts[B] is the number of
+    tokens counted, loss the balance loss."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be [T, B]")
+    T, B = logits.shape
+    elem = _elem(logits.dtype, "logits")
+    if not logits.is_cuda or (logits.stride(1) != 1 and B > 1 and T > 0):
+        raise ValueError("expected GPU logits whose rows are contiguous")
+    ld = logits.stride(0) if T > 1 else B
+    if token_mask is not None and (tuple(token_mask.shape) != (T,) or token_mask.dtype not in (torch.uint8, torch.bool)):
+        raise ValueError("token_mask must be a [T] uint8 or bool tensor")
+    dev = logits.device
+    route = _out(route, (T, B), torch.uint8, dev, "route")
+    if want_probs or probs is not None:
+        probs = _out(probs, (T, B), torch.float32, dev, "probs")
+    counts = torch.empty(B + 1, dtype=torch.int32, device=dev) if want_stats else None
+    loss = torch.empty(1, dtype=torch.float32, device=dev) if want_stats else None
+    _here(logits, token_mask, route, probs, workspace)
+    args = [logits.data_ptr(), ld, _bytes_mask(active_mask, B, "active_mask"), _dev_ptr(token_mask), T, B, int(k), elem,
+            _dev_ptr(route), _dev_ptr(probs), _dev_ptr(counts), _dev_ptr(loss)]
+    if workspace is None:
+        _check(lib.mlpmoe_route_topk(*args, _stream_ptr(stream)), "mlpmoe_route_topk")
+    else:
+        _check(lib.mlpmoe_route_topk_ws(*args, _dev_ptr(workspace), workspace.numel() * workspace.element_size(),
+                                        _stream_ptr(stream)), "mlpmoe_route_topk_ws")
+    return route, probs, counts, loss
+
+
+def mlpmoe_route_backward(probs, counts, dprobs=None, dloss=None, active_mask=None, dtype=None, dlogits=None, stream=None):
+    """Gradient of the router's logits from those of probs ([T, B] float32) and of the loss ([1] float32), either of
+    which may be None; in dtype (bfloat16 or float32, float32 if neither it nor dlogits is given)."""
+    T, B = probs.shape
+    if dtype is None:
+        dtype = torch.float32 if dlogits is None else dlogits.dtype
+    elem = _elem(dtype, "dlogits")
+    if probs.dtype != torch.float32 or (dprobs is not None and (dprobs.dtype != torch.float32 or dprobs.shape != probs.shape)):
+        raise ValueError("probs and dprobs must be [T, B] float32 tensors")
+    if dloss is not None and (dloss.dtype != torch.float32 or dloss.numel() != 1):
+        raise ValueError("dloss must be a float32 tensor of one element")
+    if counts is not None and (counts.dtype != torch.int32 or tuple(counts.shape) != (B + 1,)):
+        raise ValueError("counts must be a [B + 1] int32 tensor")
+    dlogits = _out(dlogits, (T, B), dtype, probs.device, "dlogits")
+    _here(probs, counts, dprobs, dloss, dlogits)
+    _check(lib.mlpmoe_route_backward(_dev_ptr(probs), _dev_ptr(counts), _dev_ptr(dprobs), _dev_ptr(dloss),
+                                     _bytes_mask(active_mask, B, "active_mask"), T, B, elem, _dev_ptr(dlogits),
+                                     _stream_ptr(stream)), "mlpmoe_route_backward")
+    return dlogits
+
+
+# --------------------------------------------------------------------------- 4-bit weights
+def mlpmoe_w4_quantize(W, codes=None, scales=None, stream=None):
+    """4-bit form of W [rows, cols] (bf16 or float32, cols a multiple of 32): (codes [rows, cols / 2], scales
+    [rows, cols / 32]), both uint8."""
+    rows, cols = W.shape
+    elem = _elem(W.dtype, "W")
+    codes = _out(codes, (rows, cols // 2), torch.uint8, W.device, "codes")
+    scales = _out(scales, (rows, cols // 32), torch.uint8, W.device, "scales")
+    _here(W, codes, scales)
+    _check(lib.mlpmoe_w4_quantize(_dev_ptr(W), rows, cols, elem, _dev_ptr(codes), _dev_ptr(scales), _stream_ptr(stream)),
+           "mlpmoe_w4_quantize")
+    return codes, scales
+
+
+def _w4_shape(codes, scales):
+    rows, cols = codes.shape[0], 2 * codes.shape[1]
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or tuple(scales.shape) != (rows, cols // 32):
+        raise ValueError("4-bit weights are codes [rows, cols / 2] and scales [rows, cols / 32], both uint8")
+    return rows, cols
+
+
+def mlpmoe_w4_dequantize(codes, scales, dtype=None, out=None, stream=None):
+    """The values of 4-bit weights, in bf16 (exact) or float32."""
+    rows, cols = _w4_shape(codes, scales)
+    if dtype is None:
+        dtype = torch.bfloat16 if out is None else out.dtype
+    elem = _elem(dtype, "out")
+    out = _out(out, (rows, cols), dtype, codes.device, "out")
+    _here(codes, scales, out)
+    _check(lib.mlpmoe_w4_dequantize(_dev_ptr(codes), _dev_ptr(scales), rows, cols, elem, _dev_ptr(out), _stream_ptr(stream)),
+           "mlpmoe_w4_dequantize")
+    return out
+
+
+def mlpmoe_w4_workspace_bytes(T, d_model, d_inter, B) -> int:
+    return int(lib.mlpmoe_w4_workspace_bytes(int(T), int(d_model), int(d_inter), int(B)))
+
+
+def mlpmoe_forward_w4(x, gate, up, down, branch_offsets, alpha, active_mask, route=None, out=None, out_dtype=None,
+                      workspace=None, stream=None):
+    """The forward, routed if route ([T, B] uint8) is given, on 4-bit weights: gate, up and down are the pairs
+    (codes, scales) of W_gate, W_up [d_inter, d_model] and W_down [d_model, d_inter].  x is bf16, out bf16 unless
+    out_dtype or out says float32."""
+    off, al, mk, B = _table(branch_offsets, alpha, active_mask)
+    T, d_model = x.shape
+    d_inter = int(off[-1])
+    if x.dtype != torch.bfloat16:
+        raise ValueError("x must be bfloat16")
+    if _w4_shape(*gate) != (d_inter, d_model) or _w4_shape(*up) != (d_inter, d_model) or _w4_shape(*down) != (d_model, d_inter):
+        raise ValueError("weights do not fit x and branch_offsets")
+    if route is not None and (route.dtype != torch.uint8 or tuple(route.shape) != (T, B)):
+        raise ValueError("route must be a [T, B] uint8 tensor")
+    if out_dtype is None:
+        out_dtype = torch.bfloat16 if out is None else out.dtype
+    out_bytes = _elem(out_dtype, "out")
+    out = _out(out, (T, d_model), out_dtype, x.device, "out")
+    _here(x, *gate, *up, *down, route, out, workspace)
+    args = [_dev_ptr(x), _dev_ptr(gate[0]), _dev_ptr(gate[1]), _dev_ptr(up[0]), _dev_ptr(up[1]), _dev_ptr(down[0]),
+            _dev_ptr(down[1]), off.tobytes(), al.tobytes(), mk.tobytes(), _dev_ptr(route), T, d_model, d_inter, B, out_bytes,
+            _dev_ptr(out)]
+    if workspace is None:
+        _check(lib.mlpmoe_forward_w4(*args, _stream_ptr(stream)), "mlpmoe_forward_w4")
+    else:
+        _check(lib.mlpmoe_forward_w4_ws(*args, _dev_ptr(workspace), workspace.numel() * workspace.element_size(),
+                                        _stream_ptr(stream)), "mlpmoe_forward_w4_ws")
+    return out
+
+
 class Plan:
     """A layer's branch table prepared once, with a device workspace for any T <= max_T."""
 
@@ -415,7 +597,8 @@ class Plan:
 
 KERNEL_NAMES = {1: "gate_up_mfma", 2: "down_mfma", 3: "splitk_reduce", 4: "decode_gate_up",
                 5: "decode_down", 6: "gate_up_generic", 7: "down_generic", 8: "fill_zero",
-                9: "route_tiles"}
+                9: "route_tiles", 10: "route_topk", 11: "route_finish", 12: "route_backward", 13: "w4_gate_up",
+                14: "w4_down", 15: "w4_convert"}
 
 
 def mlpmoe_profile_enable(capacity: int):

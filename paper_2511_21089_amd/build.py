@@ -16,7 +16,7 @@ BUILD_DIR = os.path.join(PKG_DIR, "_build")
 LIB_PATH = os.path.join(PKG_DIR, "libmlpmoe.so")
 
 SOURCES = ["mlpmoe_api.cpp", "kernels_generic.hip", "kernels_mfma.hip", "kernels_decode.hip",
-           "kernels_fade.hip"]
+           "kernels_fade.hip", "route_api.cpp", "kernels_route.hip", "w4_api.cpp", "kernels_w4.hip"]
 HEADERS = [os.path.join(CSRC, "internal.h"), os.path.join(ROOT, "include", "mlpmoe.h")]
 
 HIPCC = "/opt/rocm/bin/hipcc"

@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <mutex>
+
 #include "mlpmoe.h"
 
 namespace mlpmoe {
@@ -125,6 +127,55 @@ hipError_t launch_compact(const void *Wg, const void *Wu, const void *Wd, const 
                           int n_rows, int d_model, int d_inter_src, int elem_bytes, void *Wg_c,
                           void *Wu_c, void *Wd_c, hipStream_t s);
 
+// What the entry points share (mlpmoe_api.cpp): the checks of a forward's arguments, its branch table, and the current
+// device's workspace for calls that bring none (workspace_mutex held until the kernels are enqueued).
+int check_forward(const void *x, const void *Wg, const void *Wu, const void *Wd, const int32_t *off, const float *alpha,
+                  const uint8_t *mask, int T, int d_model, int d_inter, int B, const void *out);
+void make_table(const int32_t *off, const float *alpha, const uint8_t *mask, int B, BranchTable &bt);
+std::mutex &workspace_mutex();
+int owned_workspace(size_t need, size_t least, hipStream_t stream, void **ptr, size_t *bytes);
+
+// The router (kernels_route.hip).
+constexpr int kRouteMaxBlocks = 256;
+struct RouteArgs {
+    const void *logits;
+    int ld, T, B, k, elem_bytes, n_active;
+    unsigned long long active;
+    const uint8_t *token_mask;        // [T] (device), or nullptr: every token counts
+    uint8_t *route;
+    float *probs;                     // or nullptr
+    int32_t *counts;                  // [B + 1], or nullptr
+    float *loss;                      // or nullptr
+    float *part_p;                    // partial sums of more than one block
+    int *part_c;
+    hipStream_t stream;
+};
+struct RouteBackArgs {
+    const float *probs, *dprobs, *dloss;
+    const int32_t *counts;
+    int T, B, elem_bytes, n_active;
+    void *dlogits;
+    hipStream_t stream;
+};
+int route_blocks(int T, int B);
+hipError_t launch_route_topk(const RouteArgs &a);
+hipError_t launch_route_backward(const RouteBackArgs &a);
+
+// 4-bit weights (kernels_w4.hip).
+struct W4Args {
+    const void *x;
+    const uint8_t *gc, *gs, *uc, *us, *dc, *ds;      // codes and scales of W_gate, W_up, W_down
+    const uint8_t *route;             // [T, B] (device), or nullptr
+    int T, d_model, d_inter;
+    void *H;
+    int ldh;
+    void *out;
+    bool out_bf16;
+    hipStream_t stream;
+};
+hipError_t launch_w4_quantize(const void *W, size_t n, int elem_bytes, uint8_t *codes, uint8_t *scales, hipStream_t s);
+hipError_t launch_w4_dequantize(const uint8_t *codes, const uint8_t *scales, size_t n, int elem_bytes, void *W, hipStream_t s);
+hipError_t launch_w4_forward(const W4Args &a, const BranchTable &bt);
 
 // Brackets one kernel launch with a pair of events when profiling is enabled.
 void profile_mark(int kernel_id, hipStream_t s, bool begin);

@@ -228,6 +228,9 @@ int forward_impl(const void *x, const void *Wg, const void *Wu, const void *Wd, 
                          path, is_bf16, stream, nullptr, out_bf16);
 }
 
+}  // namespace
+
+namespace mlpmoe {
 // Workspace of the current device for the entry points that take none: the caller's block if one
 // was set, else the library-owned one, grown on demand.  g_ws_mutex must be held by the caller.
 // need: what a new block is made for, or least if there is not that much memory.  A block that holds least, which the call can run in, is not replaced: a graph may
@@ -279,6 +282,22 @@ int owned_workspace(size_t need, size_t least, hipStream_t stream, void **ptr, s
     *bytes = w.bytes;
     return MLPMOE_OK;
 }
+
+std::mutex &workspace_mutex() { return g_ws_mutex; }
+
+int check_forward(const void *x, const void *Wg, const void *Wu, const void *Wd, const int32_t *off, const float *alpha,
+                  const uint8_t *mask, int T, int d_model, int d_inter, int B, const void *out)
+{
+    return validate_common(x, Wg, Wu, Wd, off, alpha, mask, T, d_model, d_inter, B, static_cast<const float *>(out));
+}
+
+void make_table(const int32_t *off, const float *alpha, const uint8_t *mask, int B, BranchTable &bt)
+{
+    build_table(off, alpha, mask, B, bt);
+}
+}  // namespace mlpmoe
+
+namespace {
 
 int forward_owned(const void *x, const void *Wg, const void *Wu, const void *Wd, const int32_t *off,
                   const float *alpha, const uint8_t *mask, int T, int d_model, int d_inter, int B,
