@@ -402,11 +402,17 @@ def _forward_routed(name, x, W_gate, W_up, W_down, branch_offsets, alpha, active
 
 # --------------------------------------------------------------------------- the router
 def _here(*tensors):
-    """The tensors of a call lie on the current device, whose stream it is launched on."""
-    dev = _current_device()
+    """The addresses of a call's tensors: contiguous, on the current device, whose stream it is launched on."""
+    dev = _current_device() if torch.cuda.is_initialized() else -2
+    out = []
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
-            raise ValueError("expected GPU tensors on the current device")
+        if t is None:
+            out.append(None)
+            continue
+        if t.get_device() != dev or not t.is_contiguous():
+            raise ValueError("expected contiguous GPU tensors on the current device")
+        out.append(t.data_ptr())
+    return out
 
 
 def _bytes_mask(mask, n, what):
@@ -460,13 +466,14 @@ def mlpmoe_route_topk(logits, k, active_mask=None, token_mask=None, route=None, 
         probs = _out(probs, (T, B), torch.float32, dev, "probs")
     counts = torch.empty(B + 1, dtype=torch.int32, device=dev) if want_stats else None
     loss = torch.empty(1, dtype=torch.float32, device=dev) if want_stats else None
-    _here(logits, token_mask, route, probs, workspace)
-    args = [logits.data_ptr(), ld, _bytes_mask(active_mask, B, "active_mask"), _dev_ptr(token_mask), T, B, int(k), elem,
-            _dev_ptr(route), _dev_ptr(probs), _dev_ptr(counts), _dev_ptr(loss)]
+    ptrs = _here(token_mask, route, probs, counts, loss, workspace)
+    if logits.get_device() != _current_device():
+        raise ValueError("expected GPU tensors on the current device")
+    args = [logits.data_ptr(), ld, _bytes_mask(active_mask, B, "active_mask"), ptrs[0], T, B, int(k), elem, *ptrs[1:5]]
     if workspace is None:
         _check(lib.mlpmoe_route_topk(*args, _stream_ptr(stream)), "mlpmoe_route_topk")
     else:
-        _check(lib.mlpmoe_route_topk_ws(*args, _dev_ptr(workspace), workspace.numel() * workspace.element_size(),
+        _check(lib.mlpmoe_route_topk_ws(*args, ptrs[5], workspace.numel() * workspace.element_size(),
                                         _stream_ptr(stream)), "mlpmoe_route_topk_ws")
     return route, probs, counts, loss
 
@@ -485,9 +492,8 @@ def mlpmoe_route_backward(probs, counts, dprobs=None, dloss=None, active_mask=No
     if counts is not None and (counts.dtype != torch.int32 or tuple(counts.shape) != (B + 1,)):
         raise ValueError("counts must be a [B + 1] int32 tensor")
     dlogits = _out(dlogits, (T, B), dtype, probs.device, "dlogits")
-    _here(probs, counts, dprobs, dloss, dlogits)
-    _check(lib.mlpmoe_route_backward(_dev_ptr(probs), _dev_ptr(counts), _dev_ptr(dprobs), _dev_ptr(dloss),
-                                     _bytes_mask(active_mask, B, "active_mask"), T, B, elem, _dev_ptr(dlogits),
+    p, c, dp, dl, out = _here(probs, counts, dprobs, dloss, dlogits)
+    _check(lib.mlpmoe_route_backward(p, c, dp, dl, _bytes_mask(active_mask, B, "active_mask"), T, B, elem, out,
                                      _stream_ptr(stream)), "mlpmoe_route_backward")
     return dlogits
 
@@ -500,9 +506,8 @@ def mlpmoe_w4_quantize(W, codes=None, scales=None, stream=None):
     elem = _elem(W.dtype, "W")
     codes = _out(codes, (rows, cols // 2), torch.uint8, W.device, "codes")
     scales = _out(scales, (rows, cols // 32), torch.uint8, W.device, "scales")
-    _here(W, codes, scales)
-    _check(lib.mlpmoe_w4_quantize(_dev_ptr(W), rows, cols, elem, _dev_ptr(codes), _dev_ptr(scales), _stream_ptr(stream)),
-           "mlpmoe_w4_quantize")
+    w, c, s = _here(W, codes, scales)
+    _check(lib.mlpmoe_w4_quantize(w, rows, cols, elem, c, s, _stream_ptr(stream)), "mlpmoe_w4_quantize")
     return codes, scales
 
 
@@ -520,9 +525,8 @@ def mlpmoe_w4_dequantize(codes, scales, dtype=None, out=None, stream=None):
         dtype = torch.bfloat16 if out is None else out.dtype
     elem = _elem(dtype, "out")
     out = _out(out, (rows, cols), dtype, codes.device, "out")
-    _here(codes, scales, out)
-    _check(lib.mlpmoe_w4_dequantize(_dev_ptr(codes), _dev_ptr(scales), rows, cols, elem, _dev_ptr(out), _stream_ptr(stream)),
-           "mlpmoe_w4_dequantize")
+    c, s, w = _here(codes, scales, out)
+    _check(lib.mlpmoe_w4_dequantize(c, s, rows, cols, elem, w, _stream_ptr(stream)), "mlpmoe_w4_dequantize")
     return out
 
 
@@ -548,14 +552,12 @@ def mlpmoe_forward_w4(x, gate, up, down, branch_offsets, alpha, active_mask, rou
         out_dtype = torch.bfloat16 if out is None else out.dtype
     out_bytes = _elem(out_dtype, "out")
     out = _out(out, (T, d_model), out_dtype, x.device, "out")
-    _here(x, *gate, *up, *down, route, out, workspace)
-    args = [_dev_ptr(x), _dev_ptr(gate[0]), _dev_ptr(gate[1]), _dev_ptr(up[0]), _dev_ptr(up[1]), _dev_ptr(down[0]),
-            _dev_ptr(down[1]), off.tobytes(), al.tobytes(), mk.tobytes(), _dev_ptr(route), T, d_model, d_inter, B, out_bytes,
-            _dev_ptr(out)]
+    ptrs = _here(x, *gate, *up, *down, route, out, workspace)
+    args = [*ptrs[:7], off.tobytes(), al.tobytes(), mk.tobytes(), ptrs[7], T, d_model, d_inter, B, out_bytes, ptrs[8]]
     if workspace is None:
         _check(lib.mlpmoe_forward_w4(*args, _stream_ptr(stream)), "mlpmoe_forward_w4")
     else:
-        _check(lib.mlpmoe_forward_w4_ws(*args, _dev_ptr(workspace), workspace.numel() * workspace.element_size(),
+        _check(lib.mlpmoe_forward_w4_ws(*args, ptrs[9], workspace.numel() * workspace.element_size(),
                                         _stream_ptr(stream)), "mlpmoe_forward_w4_ws")
     return out
 

@@ -16,8 +16,8 @@ BUILD_DIR = os.path.join(PKG_DIR, "_build")
 LIB_PATH = os.path.join(PKG_DIR, "libmlpmoe.so")
 
 SOURCES = ["mlpmoe_api.cpp", "kernels_generic.hip", "kernels_mfma.hip", "kernels_decode.hip",
-           "kernels_fade.hip", "route_api.cpp", "kernels_route.hip", "w4_api.cpp", "kernels_w4.hip"]
-HEADERS = [os.path.join(CSRC, "internal.h"), os.path.join(ROOT, "include", "mlpmoe.h")]
+           "kernels_fade.hip", "route_api.cpp", "kernels_route.hip", "w4_api.cpp", "kernels_w4.hip", "kernels_w4_tiles.hip"]
+HEADERS = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "w4_common.h"), os.path.join(ROOT, "include", "mlpmoe.h")]
 
 HIPCC = "/opt/rocm/bin/hipcc"
 # packed fp32 VALU instructions are switched off for device code: the compiler would otherwise form them

@@ -39,6 +39,7 @@ struct BranchTable {
 struct BranchLanes {
     int v_next;
     float v_alpha;
+    BranchLanes() = default;
     __device__ __forceinline__ explicit BranchLanes(const BranchTable &bt)
     {
         const int lane = threadIdx.x & 63;
@@ -161,7 +162,8 @@ int route_blocks(int T, int B);
 hipError_t launch_route_topk(const RouteArgs &a);
 hipError_t launch_route_backward(const RouteBackArgs &a);
 
-// 4-bit weights (kernels_w4.hip).
+// 4-bit weights (kernels_w4.hip, kernels_w4_tiles.hip).
+constexpr int kW4MaxK = 1 << 17;      // the scales of 16 rows fit LDS beside the rest
 struct W4Args {
     const void *x;
     const uint8_t *gc, *gs, *uc, *us, *dc, *ds;      // codes and scales of W_gate, W_up, W_down
@@ -171,8 +173,11 @@ struct W4Args {
     int ldh;
     void *out;
     bool out_bf16;
+    float *partial;                   // partial sums of a K split of the down projection
     hipStream_t stream;
 };
+int w4_splits(int T, int d_model, int d_inter);
+hipError_t launch_w4_tiles(const W4Args &a, const BranchTable &bt);
 hipError_t launch_w4_quantize(const void *W, size_t n, int elem_bytes, uint8_t *codes, uint8_t *scales, hipStream_t s);
 hipError_t launch_w4_dequantize(const uint8_t *codes, const uint8_t *scales, size_t n, int elem_bytes, void *W, hipStream_t s);
 hipError_t launch_w4_forward(const W4Args &a, const BranchTable &bt);

@@ -10,244 +10,250 @@
 //   w4_down      out[t, m] = sum_n h[t, n] W_down[m, n] in float
 //
 // Both are bound by the stream of weights from HBM while few tokens share it.
-#include "internal.h"
+#include "w4_common.h"
 
 namespace mlpmoe {
 namespace {
 
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+// These kernels live for 5 to 20 us, and code that runs once is fetched as it runs, a 64-byte line in some 170 clocks: a
+// kilobyte of straight code costs as much as the latency of a load.  (The down projection with its ring of code registers
+// unrolled took 2200 clocks for a chunk of K whose data had arrived.)  So loops stay rolled, what is staged goes straight into
+// LDS without registers, and the branch table is looked at beside the first loads.
 
-__device__ const uint32_t g_zero16[4] = {0, 0, 0, 0};
+// A wave's x or H rows in LDS are 16 bytes longer than their data, so that the lanes of a cycle (eight tokens, and the piece
+// 32 dwords on) read different banks.
+constexpr int kPad = 8;
+constexpr int kRing = 4;                 // steps whose codes a wave has in flight, a kilobyte each
+constexpr int kLdsBytes = 159 * 1024;
 
-template <typename V>
-__device__ __forceinline__ V ldg(const void *p)
+// Bytes of LDS for the scales of 16 rows, as they lie in memory.
+__host__ __device__ constexpr int scale_bytes(int K) { return (K / 2 + 15) / 16 * 16 + 16; }
+
+// `bytes` of scales to LDS, `wave` of nw waves; 16 bytes a lane if base and size are multiples of 16, else 4 (they are multiples of 8).
+__device__ __forceinline__ void stage_scales(const uint8_t *src, char *dst, int bytes, bool by16, int wave, int nw)
 {
-    typedef const __attribute__((address_space(1))) V *gptr;
-    return *(gptr)p;
-}
-
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
-
-// Eight elements of a block as bf16, in order.
-__device__ __forceinline__ bf16x8 widen8(uint32_t w, float scale)
-{
-    union {
-        bf16x2 p[4];
-        bf16x8 v;
-    } r;
-    r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
-    r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
-    r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
-    r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
-    return r.v;
-}
-
-__device__ __forceinline__ float silu_mul(float g, float u)
-{
-    const float e = __builtin_amdgcn_exp2f(g * -1.4426950408889634f);
-    return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
-}
-
-__device__ __forceinline__ uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
-
-// Branches that are on and that some token of t0 .. t0 + nt - 1 takes, as a word; the same in every lane.
-__device__ __forceinline__ unsigned long long live_branches(const BranchTable &bt, const uint8_t *route, int t0, int nt)
-{
-    if (!route) return bt.active;
-    const int b = threadIdx.x & 63;
-    bool any = false;
-    if (b < bt.B)
-        for (int t = 0; t < nt; ++t) any = any || route[(size_t)(t0 + t) * bt.B + b] != 0;
-    return __ballot(any) & bt.active;
-}
-
-constexpr int kRows = 8;                 // neurons of a gate+up tile: MFMA rows 0-7 W_gate, 8-15 W_up
-constexpr int kStep = 512;               // K of a wave's step: each of its four groups of 16 lanes takes 128, four blocks
-constexpr int kPad = 8;                  // x rows in LDS are this much longer, so that 16 of them start on different banks
-
-// What a wave loads for a step: four blocks of a row a lane, and their scales.
-struct Step {
-    u32x4 w[4];
-    uint32_t s;
-};
-
-// unit: this lane's group of four blocks (128 elements) of the row; blocks: how many blocks the row has.
-__device__ __forceinline__ Step load_step(const uint8_t *codes, const uint8_t *scales, int unit, int blocks)
-{
-    Step r;
-    r.s = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int b = unit * 4 + j;
-        const bool ok = b < blocks;
-        r.w[j] = ldg<u32x4>(ok ? codes + (size_t)b * 16 : reinterpret_cast<const uint8_t *>(g_zero16));
-        r.s |= (uint32_t)ldg<uint8_t>(ok ? scales + b : reinterpret_cast<const uint8_t *>(g_zero16)) << (8 * j);
+    const int lane = threadIdx.x & 63;
+    if (by16) {
+#pragma unroll 1
+        for (int i = wave * 1024; i < bytes; i += nw * 1024)
+            if (i + lane * 16 < bytes) dma16(src + i + lane * 16, dst + i);
+    } else {
+#pragma unroll 1
+        for (int i = wave * 256; i < bytes; i += nw * 256)
+            if (i + lane * 4 < bytes)
+                __builtin_amdgcn_global_load_lds((gptr_t)(src + i + lane * 4), (lptr_t)(dst + i), 4, 0, 0);
     }
-    return r;
 }
 
-// Grid (WGs, token tiles of 16).  A wave works out tiles of 8 neurons, wave w of workgroup g the tiles w * grid + g and so on,
-// so that what live branches there are is spread over the chip.  x goes through LDS in chunks of kc.
+// Grid (workgroups, token tiles of 16).  A wave works out groups of 8 neurons, MFMA rows 0-7 W_gate and 8-15 W_up; wave w of
+// workgroup g the groups w * grid + g and so on, so that what live groups there are is spread over the chip.  x goes through
+// LDS in chunks of kc (mostly all of K), and so do the 16 rows' scales: asking for a byte a block costs as many requests as the codes
+// (4096 x 14336, gate and up codes alone 11.3 us, with a byte a block 20.8).
+template <bool kOneRun>
 __global__ void __launch_bounds__(512)
 w4_gate_up(const uint16_t *__restrict__ x, int T, int K, int kc, const uint8_t *__restrict__ gc, const uint8_t *__restrict__ gs,
            const uint8_t *__restrict__ uc, const uint8_t *__restrict__ us, uint16_t *__restrict__ H, int ldh,
-           const uint8_t *__restrict__ route, BranchTable bt)
+           const uint8_t *__restrict__ route, Range run, BranchTable bt)
 {
-    extern __shared__ __attribute__((aligned(16))) uint16_t s_x[];
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, r16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
     const int t0 = 16 * blockIdx.y, nt = T - t0 < 16 ? T - t0 : 16;
-    const unsigned long long live = live_branches(bt, route, t0, nt);
-
-    // lane b: tiles of branch b and all before it
-    const int width = lane < bt.B ? bt.off[lane + 1] - bt.off[lane] : 0;
-    int upto = (live >> lane) & 1 ? (width + kRows - 1) / kRows : 0;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int v = __shfl_up(upto, d);
-        if (lane >= d) upto += v;
+    const int blocks = K / 32, ldx = kc + kPad;
+    char *my_s = lds + nt * ldx * 2 + wave * scale_bytes(K);
+    Groups<8, kOneRun> groups(run);
+    if constexpr (kOneRun) {
+        if (blockIdx.x == 0) clear_edges(run, H + (size_t)t0 * ldh, ldh, nt, wave, nw);
+    } else {
+        __shared__ Shared sh;
+        const unsigned long long live = load_table(sh, bt, route, t0, nt);
+        groups = Groups<8, kOneRun>(sh, bt.B, live);
+        if (blockIdx.x == 0) clear_edges(sh, bt.B, live, H + (size_t)t0 * ldh, ldh, nt, wave, nw);
     }
-    const int tiles = __builtin_amdgcn_readlane(upto, 63);
 
-    // H of neurons that no token takes but that share a block of W_down's row with one that is taken has to be zero
-    if (blockIdx.x == 0)
-        for (int b = wave; b < bt.B; b += nw) {
-            if ((live >> b) & 1) continue;
-            const int lo = bt.off[b], hi = bt.off[b + 1];
-            const int end = (lo + 31) / 32 * 32 < hi ? (lo + 31) / 32 * 32 : hi;
-            const int beg = hi / 32 * 32 > end ? hi / 32 * 32 : end;
-            for (int t = 0; t < nt; ++t) {
-                if (lane < end - lo) H[(size_t)(t0 + t) * ldh + lo + lane] = 0;
-                if (lane < hi - beg) H[(size_t)(t0 + t) * ldh + beg + lane] = 0;
-            }
-        }
-
-    const int blocks = K / 32;
-    const int ldx = kc + kPad;
-    const int passes = (tiles + nw * (int)gridDim.x - 1) / (nw * (int)gridDim.x);
-    const uint16_t *xr = s_x + (r16 < nt ? r16 : 0) * ldx + q * 128;
-    for (int pass = 0; pass < passes; ++pass) {
-        const int idx = (pass * nw + wave) * gridDim.x + blockIdx.x;
-        const bool have = idx < tiles;
-        // the branch is the first whose tiles reach past idx
-        const int b = have ? __popcll(__ballot(upto <= idx)) : 0;
-        const int before = b > 0 ? __builtin_amdgcn_readlane(upto, b - 1) : 0;
-        const int n0 = have ? bt.off[b] + (idx - before) * kRows : 0;
-        const int n_end = have ? bt.off[b + 1] : 1;
-        int n = n0 + (r16 & 7);
-        n = n < n_end ? n : n_end - 1;                   // rows past the branch are computed and not stored
-        const uint8_t *codes = (r16 < 8 ? gc : uc) + (size_t)n * (K / 2);
-        const uint8_t *scales = (r16 < 8 ? gs : us) + (size_t)n * blocks;
-
+    const char *xr = lds + (r16 < nt ? r16 : 0) * ldx * 2 + q * 64;
+    const char *sc = my_s + r16 * blocks + q;
+    const int all = (K + kStepK - 1) / kStepK;
+    const int q_last = (q < blocks - (all - 1) * 4 ? q : 0) * 16;        // in the last step there may be fewer blocks than groups of lanes
+#pragma unroll 1
+    for (int at = blockIdx.x; at < groups.total; at += nw * (int)gridDim.x) {
+        const int idx = at + wave * (int)gridDim.x;
+        const bool have = idx < groups.total;
+        const int n0 = have ? groups(idx) * 8 : 0;
+        const uint8_t *codes = (r16 < 8 ? gc : uc) + (size_t)(n0 + (r16 & 7)) * (K / 2);
         f32x4 acc = {0, 0, 0, 0};
+        BranchLanes br;
+#pragma unroll 1
         for (int k0 = 0; k0 < K; k0 += kc) {
-            const int kn = K - k0 < kc ? K - k0 : kc;
-            if (pass == 0 || kc < K) {
-                __syncthreads();
-                const int pieces = (kc + 7) / 8;         // of 8 values; past K zeros
-                for (int i = threadIdx.x; i < nt * pieces; i += blockDim.x) {
-                    const int t = i / pieces, c = (i - t * pieces) * 8;
-                    u32x4 v = {0, 0, 0, 0};
-                    if (c < kn) v = ldg<u32x4>(x + (size_t)(t0 + t) * K + k0 + c);
-                    *reinterpret_cast<u32x4 *>(s_x + t * ldx + c) = v;
-                }
-                __syncthreads();
+            const int kn = K - k0 < kc ? K - k0 : kc, first = k0 / kStepK, steps = (kn + kStepK - 1) / kStepK;
+            if (k0 == 0) {
+                stage_scales(gs + (size_t)n0 * blocks, my_s, K / 4, K % 64 == 0, 0, 1);
+                stage_scales(us + (size_t)n0 * blocks, my_s + K / 4, K / 4, K % 64 == 0, 0, 1);
             }
-            if (!have) continue;
-            for (int s = 0; s * kStep < kn; ++s) {
-                const Step st = load_step(codes, scales, k0 / 128 + s * 4 + q, blocks);
+            const bool load_x = at == (int)blockIdx.x || kc < K;
+            if (load_x) {
+                if (at != (int)blockIdx.x || k0 > 0) __syncthreads();           // the last chunk has been read
+                const int per_row = kc / 512;
+#pragma unroll 1
+                for (int i = wave; i < nt * per_row; i += nw) {
+                    const int t = i / per_row, c = (i - t * per_row) * 512 + lane * 8;
+                    dma16(c < kn ? reinterpret_cast<const char *>(x + (size_t)(t0 + t) * K + k0 + c) : reinterpret_cast<const char *>(g_zero16),
+                          lds + t * ldx * 2 + (i - t * per_row) * 1024);
+                }
+            }
+            keep_order();
+            br = BranchLanes(bt);
+            u32x4 w[kRing + 1];
+            auto load = [&](int s) {                     // past the end the last one again
+                const int st = first + (s < steps ? s : steps - 1);
+                return ldg<u32x4>(codes + st * 64 + (st == all - 1 ? q_last : q * 16));
+            };
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float sc = scale_of((st.s >> (8 * j)) & 255u);
+            for (int u = 0; u < kRing; ++u) w[u] = load(u);
+            if (load_x)
+                pipeline_barrier<kRing>();
+            else
+                wait_loads<kRing>();
+            asm volatile("" : "+v"(br.v_next), "+v"(br.v_alpha));      // arrived by now: not asked for at the end
+#pragma unroll 1
+            for (int s = 0; s < steps; s += kRing + 1) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const bf16x8 xv = *reinterpret_cast<const bf16x8 *>(xr + s * kStep + j * 32 + i * 8);
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(st.w[j][i], sc), xv, acc, 0, 0, 0);
-                    }
+                for (int u = 0; u < kRing + 1; ++u) {
+                    w[(u + kRing) % (kRing + 1)] = load(s + u + kRing);
+                    if (s + u >= steps) continue;        // no way out of the loop here: loads in flight are counted through it
+                    const int b = (first + s + u) * 4;
+                    const uint32_t byte = *reinterpret_cast<const uint8_t *>(sc + b);
+                    const float scale = scale_of(b + q < blocks ? byte : 127u);      // past the end x is zero
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            widen8(w[u][j], scale), *reinterpret_cast<const bf16x8 *>(xr + (s + u) * 256 + j * 16), acc, 0, 0, 0);
                 }
             }
         }
         if (!have) continue;
-        // rows 4q .. 4q + 3 of token r16: gate in lanes q < 2, up in those 32 lanes on
-        const float alpha = bt.alpha[b];
-        const int t = t0 + r16;
-        const bool take = r16 < nt && (!route || route[(size_t)t * bt.B + b] != 0);
+        // neurons 4q .. 4q + 3 of token r16: gate in groups q < 2, up in the lanes 32 on
+        f32x4 up;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float up = __shfl_xor(acc[i], 32);
-            const int m = n0 + 4 * q + i;
-            if (q < 2 && r16 < nt && m < n_end) H[(size_t)t * ldh + m] = take ? to_bf16(alpha * silu_mul(acc[i], up)) : 0;
-        }
+        for (int i = 0; i < 4; ++i) up[i] = __shfl_xor(acc[i], 32);
+        gated<8, 1>(
+            br, bt, n0, n0 + 4 * (q & 1), [&](int, int e, float &g, float &u) { g = acc[e], u = up[e]; },
+            [&](int, int b) { return kOneRun || !route || (r16 < nt && route[(size_t)(t0 + r16) * bt.B + b] != 0); },
+            [&](int, uint2 h) {
+                if (q < 2 && r16 < nt) *reinterpret_cast<uint2 *>(H + (size_t)(t0 + r16) * ldh + h_place(n0 + 4 * q)) = h;
+            });
     }
 }
 
-constexpr int kDownWaves = 16;
-
-// Grid (tiles of 16 features, token tiles of 16).  The waves of a workgroup take turns with the steps of K, and their sums are
-// added in the order of the waves.  A block of the K axis is live if a live branch has a neuron in it; the others are not read.
-__global__ void __launch_bounds__(kDownWaves * 64)
-w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__restrict__ dc, const uint8_t *__restrict__ ds,
-        int d_model, void *__restrict__ out, int out_bf16, const uint8_t *__restrict__ route, BranchTable bt, int dense)
+// Bytes of LDS of w4_down: S stages of nt tokens' H and of codes, a kilobyte that loads without a token fill, the scales, and
+// for tables that are no single run a bit a block and the list of live steps.
+size_t down_lds(int W, int S, int nt, int K, bool one)
 {
-    extern __shared__ __attribute__((aligned(16))) uint32_t s_live[];      // a bit a block, unless all are live
-    __shared__ float red[kDownWaves][256];
+    return (size_t)S * (nt * (W * 256 + 16) + W * 1024) + 1024 + scale_bytes(K) + (one ? 0 : (size_t)ceil_div(K / 32, 32) * 4 + ceil_div(K, kStepK) * 2);
+}
+
+// Grid (tiles of 16 features, token tiles of up to 4 NL).  A workgroup of W waves owns 16 rows of W_down; in every chunk of W
+// steps of K each wave has one, so that together the waves read W * 64 bytes of a row.  Codes and H go through LDS, S - 1
+// chunks ahead.  A step is live if a live branch has a neuron in it; the others are left out.  The waves' sums are added in
+// their order.
+template <bool kOneRun, int W, int NL, int S>
+__global__ void __launch_bounds__(W * 64)
+w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__restrict__ dc, const uint8_t *__restrict__ ds,
+        int d_model, void *__restrict__ out, int out_bf16, const uint8_t *__restrict__ route, Range run, BranchTable bt)
+{
+    constexpr int PARTS = W / 4;                         // kilobytes of a token's chunk of H
+    constexpr int PER = NL + 1, AHEAD = S - 1;
+    static_assert((AHEAD - 1) * PER < 63, "loads in flight");
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, r16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int t0 = 16 * blockIdx.y, nt = T - t0 < 16 ? T - t0 : 16;
-    const int blocks = K / 32;
-    if (!dense) {
-        const unsigned long long live = live_branches(bt, route, t0, nt);
-        for (int i = threadIdx.x; i < (blocks + 31) / 32; i += blockDim.x) s_live[i] = 0;
-        __syncthreads();
-        for (int b = 0; b < bt.B; ++b) {
-            const int lo = bt.off[b], hi = bt.off[b + 1];
-            if (!((live >> b) & 1) || hi == lo) continue;
-            for (int i = lo / 32 + threadIdx.x; i <= (hi - 1) / 32; i += blockDim.x) atomicOr(&s_live[i / 32], 1u << (i & 31));
+    const int t0 = 4 * NL * blockIdx.y, nt = T - t0 < 4 * NL ? T - t0 : 4 * NL;
+    const int blocks = K / 32, all = (K + kStepK - 1) / kStepK, m0 = blockIdx.x * 16;
+    constexpr int HROW = W * 256 + 16;
+    const int stage = nt * HROW + W * 1024;
+    char *scrap = lds + S * stage, *scales = scrap + 1024;
+    uint32_t *bits = reinterpret_cast<uint32_t *>(scales + scale_bytes(K));
+    uint16_t *list = reinterpret_cast<uint16_t *>(bits + (blocks + 31) / 32);
+    stage_scales(ds + (size_t)m0 * blocks, scales, K / 2, true, wave, W);
+    const int s_beg = kOneRun ? run.beg / kStepK : 0;
+    int steps = kOneRun ? (run.end + kStepK - 1) / kStepK - s_beg : 0;
+    if constexpr (!kOneRun) {
+        __shared__ Shared sh;
+        mark_blocks(sh, bt.B, load_table(sh, bt, route, t0, nt), bits, blocks);
+        // every wave counts the live steps, and together they write the list
+#pragma unroll 1
+        for (int s = 0; s < all; s += 64) {
+            const int st = s + lane;
+            const bool on = st < all && ((bits[st / 8] >> (st % 8 * 4)) & 15u) != 0;
+            const unsigned long long m = __ballot(on);
+            if (on) list[steps + __popcll(m & ((1ULL << lane) - 1))] = (uint16_t)st;
+            steps += __popcll(m);
         }
         __syncthreads();
     }
-    const int m0 = blockIdx.x * 16;
-    const int m = m0 + r16 < d_model ? m0 + r16 : d_model - 1;
-    const uint8_t *codes = dc + (size_t)m * (K / 2), *scales = ds + (size_t)m * blocks;
-    const uint16_t *hr = H + (size_t)(t0 + (r16 < nt ? r16 : 0)) * ldh;
-    const uint8_t *zero = reinterpret_cast<const uint8_t *>(g_zero16);
+    const uint8_t *codes = dc + (size_t)(m0 + r16) * (K / 2);
+    const char *hb = reinterpret_cast<const char *>(H + (size_t)t0 * ldh);
+    // this lane's piece of a load of H: step lane >> 4 of four, piece (4 q + j) of it from place 4 j + q
+    const int h_lane = ((lane & 3) << 2 | ((lane >> 2) & 3)) * 16;
+    const int q_last = (q < blocks - (all - 1) * 4 ? q : 0) * 16;
+    auto step_of = [&](int i) { return i < steps ? (kOneRun ? s_beg + i : (int)list[i]) : -1; };
+    auto issue = [&](int c, char *dst) {                 // always PER loads
+#pragma unroll
+        for (int n = 0; n < NL; ++n) {
+            const int unit = wave * NL + n, t = unit / PARTS, part = unit % PARTS;
+            const int s = step_of(c * W + part * 4 + q);
+            const bool on = s >= 0 && t < nt;
+            dma16(on ? hb + (size_t)t * ldh * 2 + s * 256 + h_lane : reinterpret_cast<const char *>(g_zero16),
+                  t < nt ? dst + t * HROW + part * 1024 : scrap);
+        }
+        const int s = step_of(c * W + wave);
+        dma16(s >= 0 ? reinterpret_cast<const char *>(codes + s * 64 + (s == all - 1 ? q_last : q * 16)) : reinterpret_cast<const char *>(g_zero16),
+              dst + nt * HROW + wave * 1024);
+    };
+    const int chunks = (steps + W - 1) / W;
+    keep_order();
+#pragma unroll 1
+    for (int c = 0; c < AHEAD; ++c) issue(c, lds + c * stage);
     f32x4 acc = {0, 0, 0, 0};
-    for (int s = wave; s * kStep < K; s += kDownWaves) {
-        const int unit = s * 4 + q;
-        unsigned ok = 0;
-        if (unit * 4 < blocks) ok = dense ? 15u : (s_live[unit / 8] >> (unit % 8 * 4)) & 15u;
-        if (blocks - unit * 4 < 4 && ok) ok &= (1u << (blocks - unit * 4)) - 1u;
-        if (__ballot(ok != 0) == 0) continue;
+    const char *mine = lds, *end = lds + S * stage;
+    char *fill = lds + AHEAD * stage;
+    const int hr = (r16 < nt ? r16 : 0) * HROW + wave * 256 + q * 64, wr = nt * HROW + wave * 1024 + lane * 16;
+#pragma unroll 1
+    for (int c = 0; c < chunks; ++c) {
+        pipeline_barrier<(AHEAD - 1) * PER>();
+        issue(c + AHEAD, fill);
+        const int s = step_of(c * W + wave);
+        if (s >= 0) {
+            const int b = s * 4 + q;
+            const uint32_t byte = *reinterpret_cast<const uint8_t *>(scales + r16 * blocks + b);
+            // a block that is not live: H is zero there, the scale may be no number
+            const bool on = b < blocks && (kOneRun ? b >= run.beg / 32 && b * 32 < run.end : (bits[b / 32] >> (b & 31) & 1) != 0);
+            const float scale = scale_of(on ? byte : 127u);
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(mine + wr);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const bool on = (ok >> j) & 1u;
-            const int b = unit * 4 + j;
-            const u32x4 w = ldg<u32x4>(on ? codes + (size_t)b * 16 : zero);
-            const float sc = scale_of(ldg<uint8_t>(on ? scales + b : zero));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bf16x8 hv = ldg<bf16x8>(on ? reinterpret_cast<const uint8_t *>(hr + b * 32 + i * 8) : zero);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[i], sc), hv, acc, 0, 0, 0);
-            }
+            for (int j = 0; j < 4; ++j)
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[j], scale), *reinterpret_cast<const bf16x8 *>(mine + hr + j * 16),
+                                                              acc, 0, 0, 0);
         }
+        mine = mine + stage == end ? lds : mine + stage;
+        fill = fill + stage == end ? lds : fill + stage;
     }
+    pipeline_barrier<0>();
+    float *red = reinterpret_cast<float *>(lds);         // where the stages were
 #pragma unroll
-    for (int i = 0; i < 4; ++i) red[wave][r16 * 16 + 4 * q + i] = acc[i];
+    for (int i = 0; i < 4; ++i) red[wave * 256 + r16 * 16 + 4 * q + i] = acc[i];
     __syncthreads();
     if (threadIdx.x < 256) {
         const int t = threadIdx.x >> 4, f = m0 + (threadIdx.x & 15);
         float v = 0;
 #pragma unroll
-        for (int w = 0; w < kDownWaves; ++w) v += red[w][threadIdx.x];
-        if (t < nt && f < d_model) {
-            const size_t at = (size_t)(t0 + t) * d_model + f;
+        for (int w = 0; w < W; ++w) v += red[w * 256 + threadIdx.x];
+        if (t < nt) {
+            const size_t to = (size_t)(t0 + t) * d_model + f;
             if (out_bf16)
-                static_cast<uint16_t *>(out)[at] = to_bf16(v);
+                static_cast<uint16_t *>(out)[to] = to_bf16(v);
             else
-                static_cast<float *>(out)[at] = v;
+                static_cast<float *>(out)[to] = v;
         }
     }
 }
@@ -321,8 +327,34 @@ unsigned convert_blocks(size_t pieces)
     return (unsigned)(want < 8192 ? want : 8192);
 }
 
-// Bytes of LDS for x: all of K if 16 rows (fewer for fewer tokens) fit, else chunks.
-constexpr int kXBytes = 144 * 1024;
+size_t gate_up_lds(int nt, int nw, int kc, int K) { return (size_t)nt * (kc + kPad) * 2 + (size_t)nw * scale_bytes(K); }
+
+template <bool kOneRun, int W, int NL, int S>
+hipError_t launch_down(const W4Args &a, const BranchTable &bt, const Range &run)
+{
+    const int nt = a.T < 4 * NL ? a.T : 4 * NL;
+    const size_t lds = down_lds(W, S, nt, a.d_inter, kOneRun);
+    const hipError_t e = allow_lds<w4_down<kOneRun, W, NL, S>>((int)lds, "w4_down attribute");
+    if (e != hipSuccess) return e;
+    ProfileScope ps(MLPMOE_KERNEL_W4_DOWN, a.stream);
+    w4_down<kOneRun, W, NL, S><<<dim3(a.d_model / 16, ceil_div(a.T, 4 * NL)), W * 64, lds, a.stream>>>(
+        static_cast<const uint16_t *>(a.H), a.ldh, a.T, a.d_inter, a.dc, a.ds, a.d_model, a.out, a.out_bf16, a.route, run, bt);
+    return launch_status("w4_down launch");
+}
+
+// 16 waves while three stages of their chunks fit, else 8, whose chunks are half as long.
+template <bool kOneRun>
+hipError_t down(const W4Args &a, const BranchTable &bt, const Range &run)
+{
+    const int nt = a.T < 16 ? a.T : 16, K = a.d_inter;
+    auto fits = [&](int W, int S) { return down_lds(W, S, nt, K, kOneRun) <= (size_t)kLdsBytes; };
+    if (nt == 1 && fits(16, 7)) return launch_down<kOneRun, 16, 1, 7>(a, bt, run);
+    if (nt <= 4 && fits(16, 4)) return launch_down<kOneRun, 16, 1, 4>(a, bt, run);
+    if (nt <= 8 && fits(16, 3)) return launch_down<kOneRun, 16, 2, 3>(a, bt, run);
+    if (nt <= 12 && fits(8, 4)) return launch_down<kOneRun, 8, 3, 4>(a, bt, run);
+    if (fits(8, 3)) return launch_down<kOneRun, 8, 4, 3>(a, bt, run);
+    return launch_down<kOneRun, 8, 1, 3>(a, bt, run);    // scales of a very long K: four tokens at a time
+}
 
 }  // namespace
 
@@ -353,33 +385,33 @@ hipError_t launch_w4_dequantize(const uint8_t *codes, const uint8_t *scales, siz
 
 hipError_t launch_w4_forward(const W4Args &a, const BranchTable &bt)
 {
-    const int nt = a.T < 16 ? a.T : 16, token_tiles = ceil_div(a.T, 16);
-    int kc = (kXBytes / (2 * nt) - kPad) / kStep * kStep;
-    const int k_all = ceil_div(a.d_model, kStep) * kStep;
-    if (kc > k_all) kc = k_all;
-    int tiles = 0;
+    const int nt = a.T < 16 ? a.T : 16, token_tiles = ceil_div(a.T, 16), cus = 256;
+    const bool one = !a.route && bt.n_runs == 1;
+    const Range run = one ? Range{bt.run_start[0], bt.run_end[0]} : Range{0, 0};
+    int groups = 0;                          // an upper bound: a group shared by two branches counts for both
     for (int b = 0; b < bt.B; ++b)
-        if ((bt.active >> b) & 1) tiles += ceil_div(bt.off[b + 1] - bt.off[b], kRows);
-    const int nw = 8;
-    int grid = ceil_div(tiles, nw);
-    const size_t lds = (size_t)nt * (kc + kPad) * 2;
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(w4_gate_up), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                       160 * 1024);
-    if (e != hipSuccess) return note_hip_error("w4_gate_up attribute", e);
+        if (((bt.active >> b) & 1) && bt.off[b + 1] > bt.off[b]) groups += ceil_div(bt.off[b + 1], 8) - bt.off[b] / 8;
+    if (one) groups = ceil_div(run.end, 8) - run.beg / 8;
+    int nw = ceil_div(groups, cus);
+    if (nw > 8) nw = 8;
+    while (nw > 1 && gate_up_lds(nt, nw, 512, a.d_model) > (size_t)kLdsBytes) --nw;
+    int kc = ceil_div(a.d_model, 512) * 512;
+    while (gate_up_lds(nt, nw, kc, a.d_model) > (size_t)kLdsBytes) kc = ceil_div(kc / 2, 512) * 512;
+    const size_t lds = gate_up_lds(nt, nw, kc, a.d_model);
+    const int resident = cus * (lds > 78 * 1024 ? 1 : lds > 39 * 1024 ? 2 : 4);
+    int grid = ceil_div(groups, nw);
+    if (grid > resident) grid = resident;
+    hipError_t e = one ? allow_lds<w4_gate_up<true>>((int)lds, "w4_gate_up attribute") : allow_lds<w4_gate_up<false>>((int)lds, "w4_gate_up attribute");
+    if (e != hipSuccess) return e;
     {
         ProfileScope ps(MLPMOE_KERNEL_W4_GATE_UP, a.stream);
-        w4_gate_up<<<dim3(grid, token_tiles), nw * 64, lds, a.stream>>>(static_cast<const uint16_t *>(a.x), a.T, a.d_model, kc, a.gc,
-                                                                    a.gs, a.uc, a.us, static_cast<uint16_t *>(a.H), a.ldh,
-                                                                    a.route, bt);
+        (one ? w4_gate_up<true> : w4_gate_up<false>)<<<dim3(grid, token_tiles), nw * 64, lds, a.stream>>>(
+            static_cast<const uint16_t *>(a.x), a.T, a.d_model, kc, a.gc, a.gs, a.uc, a.us, static_cast<uint16_t *>(a.H), a.ldh, a.route, run,
+            bt);
         e = launch_status("w4_gate_up launch");
         if (e != hipSuccess) return e;
     }
-    const bool dense = !a.route && bt.d_eff == a.d_inter;
-    const size_t bits = dense ? 0 : (size_t)ceil_div(a.d_inter / 32, 32) * 4;
-    ProfileScope ps(MLPMOE_KERNEL_W4_DOWN, a.stream);
-    w4_down<<<dim3(ceil_div(a.d_model, 16), token_tiles), kDownWaves * 64, bits, a.stream>>>(
-        static_cast<const uint16_t *>(a.H), a.ldh, a.T, a.d_inter, a.dc, a.ds, a.d_model, a.out, a.out_bf16, a.route, bt, dense);
-    return launch_status("w4_down launch");
+    return one ? down<true>(a, bt, run) : down<false>(a, bt, run);
 }
 
 }  // namespace mlpmoe

@@ -9,6 +9,10 @@ namespace {
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// H of the kernels on 4-bit weights: rows of whole steps of K (128).
+int w4_h_ld(int d_inter) { return (int)align_up((size_t)d_inter, 128); }
+size_t h_bytes(int T, int d_inter) { return align_up((size_t)T * w4_h_ld(d_inter) * 2, 256); }
+
 int check_matrix(const void *codes, const void *scales, const void *W, int rows, int cols, int elem_bytes)
 {
     if (rows < 0 || cols < 1 || rows > (1 << 22) || cols > (1 << 22) || (long long)rows * cols > (1LL << 40)) return MLPMOE_ERR_SHAPE;
@@ -25,7 +29,8 @@ int forward_w4(const void *x, const uint8_t *const w[6], const int32_t *off, con
 {
     int rc = check_forward(x, w[0], w[2], w[4], off, alpha, mask, T, d_model, d_inter, B, out);
     if (rc != MLPMOE_OK) return rc;
-    if ((out_bytes != 2 && out_bytes != 4) || d_model % 32 != 0 || d_inter % 32 != 0) return MLPMOE_ERR_UNSUPPORTED;
+    if ((out_bytes != 2 && out_bytes != 4) || d_model % 32 != 0 || d_inter % 32 != 0 || d_model > kW4MaxK || d_inter > kW4MaxK)
+        return MLPMOE_ERR_UNSUPPORTED;
     if (T == 0) return MLPMOE_OK;
     if (d_inter > 0 && (!w[1] || !w[3] || !w[5])) return MLPMOE_ERR_NULL;
     if (!aligned16(w[1]) || !aligned16(w[3]) || !aligned16(w[5])) return MLPMOE_ERR_ALIGN;
@@ -56,11 +61,12 @@ int forward_w4(const void *x, const uint8_t *const w[6], const int32_t *off, con
     a.route = route;
     a.T = T; a.d_model = d_model; a.d_inter = d_inter;
     a.H = workspace;
-    a.ldh = h_ld(d_inter);
+    a.ldh = w4_h_ld(d_inter);
     a.out = out;
     a.out_bf16 = out_bytes == 2;
+    a.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + h_bytes(T, d_inter));
     a.stream = s;
-    const hipError_t e = launch_w4_forward(a, bt);
+    const hipError_t e = T > 16 ? launch_w4_tiles(a, bt) : launch_w4_forward(a, bt);
     if (e != hipSuccess && g_err_detail[0] == 0) (void)note_hip_error("kernel launch", e);
     return e == hipSuccess ? MLPMOE_OK : MLPMOE_ERR_HIP;
 }
@@ -92,7 +98,8 @@ int mlpmoe_w4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, 
 size_t mlpmoe_w4_workspace_bytes(int T, int d_model, int d_inter, int B)
 {
     if (T < 0 || d_model < 1 || d_inter < 0 || B < 1 || B > MLPMOE_MAX_BRANCHES) return 0;
-    return align_up((size_t)T * h_ld(d_inter) * 2, 256) + 256;
+    const int splits = T > 16 ? w4_splits(T, d_model, d_inter) : 1;
+    return h_bytes(T, d_inter) + (splits > 1 ? align_up((size_t)splits * T * d_model * 4, 256) : 0) + 256;
 }
 
 int mlpmoe_forward_w4(const void *x, const uint8_t *gate_codes, const uint8_t *gate_scales, const uint8_t *up_codes,

@@ -1,0 +1,279 @@
+// Device code that the kernels on 4-bit weights share.
+#pragma once
+
+#include <mutex>
+
+#include "internal.h"
+
+namespace mlpmoe {
+namespace {
+
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(4), aligned(1))) uint32_t u32x4_any;      // at any address
+
+typedef const __attribute__((address_space(1))) void *gptr_t;
+typedef __attribute__((address_space(3))) void *lptr_t;
+
+__device__ const uint32_t g_zero16[4] = {0, 0, 0, 0};
+
+template <typename V>
+__device__ __forceinline__ V ldg(const void *p)
+{
+    typedef const __attribute__((address_space(1))) V *gptr;
+    return *(gptr)p;
+}
+
+// One wave-wide load of 16 bytes a lane straight into LDS: lane l's data lands at dst + 16 l.
+__device__ __forceinline__ void dma16(const void *src, void *dst)
+{
+    __builtin_amdgcn_global_load_lds((gptr_t)src, (lptr_t)dst, 16, 0, 0);
+}
+
+// No memory operation moves across: the counted waits below rely on the order in which loads are issued.
+__device__ __forceinline__ void keep_order()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Waits until at most N of this wave's loads are outstanding (they return in issue order) and none of its LDS operations.
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+// ... and then for the workgroup's other waves.  Written by hand because the compiler's own barrier waits for every load.
+template <int N>
+__device__ __forceinline__ void pipeline_barrier()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+
+// Eight elements of a block as bf16, in order.
+__device__ __forceinline__ bf16x8 widen8(uint32_t w, float scale)
+{
+    union {
+        bf16x2 p[4];
+        bf16x8 v;
+    } r;
+    r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
+    r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+    r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
+    r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+    return r.v;
+}
+
+__device__ __forceinline__ float silu_mul(float g, float u)
+{
+    const float e = __builtin_amdgcn_exp2f(g * -1.4426950408889634f);
+    return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
+}
+
+__device__ __forceinline__ uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+
+// K goes by steps of 128: a lane's 16 bytes of codes are a block of 32, group q = lane >> 4 takes block q of the step, and the
+// j-th of the step's four MFMAs elements 8 j .. 8 j + 7 of it.  So a step's 16 pieces of x or H (8 values, 16 bytes) are read as
+// piece 4 q + j by group q.  H lies in memory with the pieces of every 128 in the order in which they are read, 4 j + q, so
+// that the four groups of a load read 64 bytes in a row; x, the caller's, is put in order in LDS.
+constexpr int kStepK = 128;
+
+// Place of neuron n in a row of H.
+__device__ __forceinline__ int h_place(int n) { return (n & ~127) | ((n >> 3) & 3) << 5 | ((n >> 5) & 3) << 3 | (n & 7); }
+
+// 16 bytes of scales, as they are loaded: from p, or from the last 16 of the matrix if p is nearer to its end.  No branch, so
+// that nothing waits for the load before place() does.  Scales of blocks past a row's end are those of the next row: their
+// lanes have codes of 0 and take a scale of 1.
+struct ScalePiece {
+    u32x4 v;
+    int late;                // bytes that p lies behind where the load began
+    __device__ __forceinline__ void load(const uint8_t *p, const uint8_t *end)
+    {
+        const long long over = p + 16 - end;
+        late = over > 0 ? (int)(over < 16 ? over : 16) : 0;
+        v = ldg<u32x4_any>(over > 0 ? end - 16 : p);
+    }
+    __device__ __forceinline__ void place(char *lds) const
+    {
+        u32x4 r = v;
+        if (__ballot(late > 0)) {
+            const int d = late >> 2, b = late & 3;
+            const uint32_t x[8] = {v.x, v.y, v.z, v.w, 0, 0, 0, 0};
+            uint32_t y[5];
+#pragma unroll
+            for (int i = 0; i < 5; ++i) y[i] = d == 0 ? x[i] : d == 1 ? x[i + 1] : d == 2 ? x[i + 2] : i + 3 < 8 && d == 3 ? x[i + 3] : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_alignbyte(y[i + 1], y[i], b);
+        }
+        *reinterpret_cast<u32x4 *>(lds) = r;
+    }
+};
+
+// The neurons of a call's live branches (on, and some token of the workgroup's takes them).  Mostly they are one range that the
+// host knows (kOneRun: no routing, one run of active branches); a workgroup then asks for weights at once, without having seen
+// the table, whose arguments take a round trip.  Otherwise the table and the routes are looked through first, and what comes
+// of it is kept in LDS.
+struct Range {
+    int beg, end;
+};
+
+struct Shared {
+    int off[MLPMOE_MAX_BRANCHES + 1];
+    unsigned any[2];
+};
+
+// Live branches of the tokens t0 .. t0 + nt - 1, and the offsets into LDS.  Ends with a barrier.
+__device__ __forceinline__ unsigned long long load_table(Shared &sh, const BranchTable &bt, const uint8_t *route, int t0, int nt)
+{
+    const int tid = threadIdx.x;
+    if (tid < 2) sh.any[tid] = 0;
+    for (int i = tid; i <= MLPMOE_MAX_BRANCHES; i += blockDim.x) sh.off[i] = bt.off[i];
+    __syncthreads();
+    if (!route) return bt.active;
+    for (int i = tid; i < nt * bt.B; i += blockDim.x) {
+        const int b = i % bt.B;
+        if (route[(size_t)t0 * bt.B + i]) atomicOr(&sh.any[b >> 5], 1u << (b & 31));
+    }
+    __syncthreads();
+    return (sh.any[0] | ((unsigned long long)sh.any[1] << 32)) & bt.active;
+}
+
+// The groups of G neurons, at multiples of G, that a live branch reaches into, numbered in order.
+template <int G, bool kOneRun>
+struct Groups {
+    int beg, upto;           // lane b: first group that branch b adds to those of the live branches before it; their number with it
+    int total;
+    __device__ __forceinline__ Groups(const Range &run) : beg(run.beg / G), upto(0), total((run.end + G - 1) / G - run.beg / G) {}
+    __device__ __forceinline__ Groups(const Shared &sh, int B, unsigned long long live)
+    {
+        const int lane = threadIdx.x & 63;
+        const bool on = lane < B && ((live >> lane) & 1);
+        const int lo = on ? sh.off[lane] : 0, hi = on ? sh.off[lane + 1] : 0;
+        int end = hi > lo ? (hi + G - 1) / G : 0;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int v = __shfl_up(end, d);
+            if (lane >= d && v > end) end = v;
+        }
+        int before = __shfl_up(end, 1);
+        if (lane == 0) before = 0;
+        beg = lo / G > before ? lo / G : before;
+        upto = hi > lo ? end - beg : 0;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int v = __shfl_up(upto, d);
+            if (lane >= d) upto += v;
+        }
+        total = __builtin_amdgcn_readlane(upto, 63);
+    }
+    // group number i (uniform, i < total)
+    __device__ __forceinline__ int operator()(int i) const
+    {
+        if (kOneRun) return beg + i;
+        const int b = __popcll(__ballot(upto <= i));
+        return __builtin_amdgcn_readlane(beg, b) + i - (b > 0 ? __builtin_amdgcn_readlane(upto, b - 1) : 0);
+    }
+};
+
+// h of 4 neurons n .. n + 3 (this lane's) of a group n0 .. n0 + G - 1 (uniform) for F tokens, as bf16: alpha SiLU(g) u, or 0 where the
+// neuron's branch is off or the token does not take it.  store(token, 8 bytes).  All lanes of the wave call it.
+template <int G, int F, typename Value, typename Takes, typename Store>
+__device__ __forceinline__ void gated(const BranchLanes &br, const BranchTable &bt, int n0, int n, Value value, Takes takes, Store store)
+{
+    const int b0 = br.branch(n0);
+    const bool one = br.next(b0) >= n0 + G;             // the whole group is in one branch
+    const float alpha0 = br.alpha(b0);
+    const bool on0 = (bt.active >> b0) & 1;
+    float alpha[4];
+    int branch[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) alpha[e] = alpha0, branch[e] = on0 ? b0 : -1;
+    if (!one)
+        for (int b = b0 + 1, beg = br.next(b0); beg < n0 + G; beg = br.next(b), ++b) {
+            const float a = br.alpha(b);
+            const bool on = (bt.active >> b) & 1;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e >= beg) alpha[e] = a, branch[e] = on ? b : -1;
+        }
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+        uint16_t h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float g, u;
+            value(f, e, g, u);
+            h[e] = branch[e] >= 0 && takes(f, branch[e]) ? to_bf16(alpha[e] * silu_mul(g, u)) : (uint16_t)0;
+        }
+        store(f, uint2{(uint32_t)h[0] | (uint32_t)h[1] << 16, (uint32_t)h[2] | (uint32_t)h[3] << 16});
+    }
+}
+
+// The down projection reads H by whole steps of 128 neurons.  Groups of G that a live branch reaches into are written whole;
+// here the rest of such a step is set to zero.  wave of nw: the work is shared out.
+__device__ __forceinline__ void clear_range(uint16_t *H, int ldh, int nt, int from, int to, int wave, int nw)
+{
+    for (int t = wave; t < nt; t += nw)
+        for (int n = from + (threadIdx.x & 63); n < to; n += 64) H[(size_t)t * ldh + h_place(n)] = 0;
+}
+__device__ __forceinline__ void clear_edges(const Range &run, uint16_t *H, int ldh, int nt, int wave, int nw)
+{
+    if (run.beg % kStepK) clear_range(H, ldh, nt, run.beg / kStepK * kStepK, run.beg, wave, nw);
+    if (run.end % kStepK) clear_range(H, ldh, nt, run.end, (run.end + kStepK - 1) / kStepK * kStepK, wave, nw);
+}
+__device__ __forceinline__ void clear_edges(const Shared &sh, int B, unsigned long long live, uint16_t *H, int ldh, int nt, int wave,
+                                            int nw)
+{
+    for (int b = 0; b <= B; ++b) {                       // past the last branch: the rest of its step
+        const int from = sh.off[b], to = b < B ? sh.off[b + 1] : ldh;
+        if ((b < B && ((live >> b) & 1)) || to == from) continue;
+        const int up = (from + kStepK - 1) / kStepK * kStepK, down = to / kStepK * kStepK;
+        const int end = up < to ? up : to, beg = down > end ? down : end;
+        clear_range(H, ldh, nt, from, end, wave, nw);
+        clear_range(H, ldh, nt, beg, to, wave, nw);
+    }
+}
+
+// A bit a block of the K axis of W_down: whether a live branch has a neuron in it.  Ends with a barrier.
+__device__ __forceinline__ void mark_blocks(const Shared &sh, int B, unsigned long long live, uint32_t *bits, int blocks)
+{
+    for (int i = threadIdx.x; i < (blocks + 31) / 32; i += blockDim.x) bits[i] = 0;
+    __syncthreads();
+    for (int b = 0; b < B; ++b) {
+        const int lo = sh.off[b], hi = sh.off[b + 1];
+        if (!((live >> b) & 1) || hi == lo) continue;
+        for (int i = lo / 32 + threadIdx.x; i <= (hi - 1) / 32; i += blockDim.x) atomicOr(&bits[i / 32], 1u << (i & 31));
+    }
+    __syncthreads();
+}
+
+// Lets a kernel have `bytes` of LDS on the current device: the runtime is asked when a call needs more than those before it
+// (2 us a call otherwise, of 8 for a launch or two).
+template <auto kernel>
+hipError_t allow_lds(int bytes, const char *what)
+{
+    static std::mutex mu;
+    static int given[64] = {0};
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return note_hip_error("hipGetDevice", e);
+    if (dev < 0 || dev >= 64) return note_hip_error("device index", hipErrorInvalidDevice);
+    std::lock_guard<std::mutex> lock(mu);
+    if (given[dev] >= bytes) return hipSuccess;
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return note_hip_error(what, e);
+    given[dev] = bytes;
+    return hipSuccess;
+}
+
+}  // namespace
+}  // namespace mlpmoe
