@@ -20,10 +20,6 @@ namespace {
 // unrolled took 2200 clocks for a chunk of K whose data had arrived.)  So loops stay rolled, what is staged goes straight into
 // LDS without registers, and the branch table is looked at beside the first loads.
 
-// A wave's x or H rows in LDS are 16 bytes longer than their data, so that the lanes of a cycle (eight tokens, and the piece
-// 32 dwords on) read different banks.
-constexpr int kPad = 8;
-constexpr int kRing = 4;                 // steps whose codes a wave has in flight, a kilobyte each
 constexpr int kLdsBytes = 159 * 1024;
 
 // Bytes of LDS for the scales of 16 rows, as they lie in memory.
@@ -45,97 +41,124 @@ __device__ __forceinline__ void stage_scales(const uint8_t *src, char *dst, int 
     }
 }
 
-// Grid (workgroups, token tiles of 16).  A wave works out groups of 8 neurons, MFMA rows 0-7 W_gate and 8-15 W_up; wave w of
-// workgroup g the groups w * grid + g and so on, so that what live groups there are is spread over the chip.  x goes through
-// LDS in chunks of kc (mostly all of K), and so do the 16 rows' scales: asking for a byte a block costs as many requests as the codes
-// (4096 x 14336, gate and up codes alone 11.3 us, with a byte a block 20.8).
-template <bool kOneRun>
+constexpr int kChunkK = 512;             // K of a stage of w4_gate_up: four steps
+constexpr int kXRow = kChunkK * 2 + 16;  // bytes of a token's x in it: the lanes of a cycle (eight tokens, two pieces 8 apart) read different banks
+
+// Bytes of LDS: S stages, x of nt tokens in each of them or, whole, beside them.
+size_t gate_up_lds(int nt, int nw, int S, int K, bool whole)
+{
+    return (size_t)S * nw * 4096 + (size_t)(whole ? ceil_div(K, kChunkK) : S) * nt * kXRow + 1024 + (size_t)nw * scale_bytes(K);
+}
+
+// Grid (workgroups, tiles of tt tokens).  A wave works out groups of 8 neurons, MFMA rows 0-7 W_gate and 8-15 W_up; wave w of
+// workgroup g the groups w * grid + g and so on, so that what live groups there are is spread over the chip.
+// 512 of K at a time, the codes (each wave its own) go through LDS, S - 1 stages ahead, and with them x (for the workgroup), which
+// has the waves meet for every stage; XL = 0: x fits LDS whole, and after one meeting every wave goes at its own pace.  A load of codes
+// is 256 bytes of four rows each: 4096 x 14336, gate and up codes alone, 10.2 us, and 11.3 us with 64 bytes of 16 rows.  Row r's 16-byte
+// piece c lies at place c ^ r of its 256 bytes, and group q of lanes takes piece (block) 4 q + s in step s, so that the lanes of a
+// cycle read different banks; x lies in the order in which it is read.  The 16 rows' scales are staged whole: asking for a byte
+// a block costs as many requests as the codes (20.8 us).
+template <bool kOneRun, int XL, int S>
 __global__ void __launch_bounds__(512)
-w4_gate_up(const uint16_t *__restrict__ x, int T, int K, int kc, const uint8_t *__restrict__ gc, const uint8_t *__restrict__ gs,
+w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *__restrict__ gc, const uint8_t *__restrict__ gs,
            const uint8_t *__restrict__ uc, const uint8_t *__restrict__ us, uint16_t *__restrict__ H, int ldh,
            const uint8_t *__restrict__ route, Range run, BranchTable bt)
 {
+    constexpr int PER = 4 + XL, AHEAD = S - 1;
+    static_assert((AHEAD - 1) * PER < 63, "loads in flight");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, r16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
-    const int t0 = 16 * blockIdx.y, nt = T - t0 < 16 ? T - t0 : 16;
-    const int blocks = K / 32, ldx = kc + kPad;
-    char *my_s = lds + nt * ldx * 2 + wave * scale_bytes(K);
+    const int t0 = tt * blockIdx.y, nt = T - t0 < tt ? T - t0 : tt;
+    const int blocks = K / 32, chunks = (K + kChunkK - 1) / kChunkK;
+    constexpr bool kWhole = XL == 0;
+    const int stage = (kWhole ? 0 : nt * kXRow) + nw * 4096;
+    char *all_x = lds + S * stage, *scrap = all_x + (kWhole ? chunks * nt * kXRow : 0), *my_s = scrap + 1024 + wave * scale_bytes(K);
     Groups<8, kOneRun> groups(run);
     if constexpr (kOneRun) {
         if (blockIdx.x == 0) clear_edges(run, H + (size_t)t0 * ldh, ldh, nt, wave, nw);
     } else {
-        __shared__ Shared sh;
-        const unsigned long long live = load_table(sh, bt, route, t0, nt);
-        groups = Groups<8, kOneRun>(sh, bt.B, live);
-        if (blockIdx.x == 0) clear_edges(sh, bt.B, live, H + (size_t)t0 * ldh, ldh, nt, wave, nw);
+        const OffsetLanes off(bt);
+        const unsigned long long live = live_of_16(bt, route, t0, nt);
+        groups = Groups<8, kOneRun>(off, live);
+        if (blockIdx.x == 0) clear_edges(off, bt.B, live, H + (size_t)t0 * ldh, ldh, nt, wave, nw);
     }
 
-    const char *xr = lds + (r16 < nt ? r16 : 0) * ldx * 2 + q * 64;
-    const char *sc = my_s + r16 * blocks + q;
-    const int all = (K + kStepK - 1) / kStepK;
-    const int q_last = (q < blocks - (all - 1) * 4 ? q : 0) * 16;        // in the last step there may be fewer blocks than groups of lanes
+    // lane of a load of x: place 16 s + 4 q + j of the 64 is piece 16 q + 4 s + j
+    const int x_piece = ((lane >> 2) & 3) * 16 + (lane >> 4) * 4 + (lane & 3);
+    const char *zero = reinterpret_cast<const char *>(g_zero16);
+    const int xr = (r16 < nt ? r16 : 0) * kXRow + q * 64, cb = (kWhole ? 0 : nt * kXRow) + wave * 4096;
 #pragma unroll 1
     for (int at = blockIdx.x; at < groups.total; at += nw * (int)gridDim.x) {
         const int idx = at + wave * (int)gridDim.x;
         const bool have = idx < groups.total;
         const int n0 = have ? groups(idx) * 8 : 0;
-        const uint8_t *codes = (r16 < 8 ? gc : uc) + (size_t)(n0 + (r16 & 7)) * (K / 2);
-        f32x4 acc = {0, 0, 0, 0};
-        BranchLanes br;
+        if (at != (int)blockIdx.x) pipeline_barrier<0>();               // the last group's stages and scales have been read
+        const char *xb = reinterpret_cast<const char *>(x + (size_t)t0 * K);
+        const uint8_t *gb = gc + (size_t)n0 * (K / 2), *ub = uc + (size_t)n0 * (K / 2);
+        auto issue = [&](int c, char *dst) {             // always PER loads; past the end the last chunk again
+            const int k = c < chunks ? c : chunks - 1;
+#pragma unroll
+            for (int n = 0; n < XL; ++n) {
+                const int t = wave + n * nw;
+                dma16(t < nt && k * 64 + x_piece < K / 8 ? xb + (size_t)t * K * 2 + k * 1024 + x_piece * 16 : zero, t < nt ? dst + t * kXRow : scrap);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int piece = r16 ^ (4 * i + q);     // of row 4 i + q; past the row's end, where x is zero, its first
+                const int off = (4 * (i & 1) + q) * (K / 2) + (k * 16 + piece < blocks ? k * 16 + piece : 0) * 16;
+                dma16(have ? reinterpret_cast<const char *>((i < 2 ? gb : ub) + off) : zero, dst + cb + i * 1024);
+            }
+        };
+        keep_order();
 #pragma unroll 1
-        for (int k0 = 0; k0 < K; k0 += kc) {
-            const int kn = K - k0 < kc ? K - k0 : kc, first = k0 / kStepK, steps = (kn + kStepK - 1) / kStepK;
-            if (k0 == 0) {
+        for (int c = 0; c < AHEAD; ++c) {
+            issue(c, lds + c * stage);
+            if (c == 0) {
+                if (kWhole && at == (int)blockIdx.x)
+#pragma unroll 1
+                    for (int u = wave; u < nt * chunks; u += nw) {
+                        const int k = u / nt, t = u - k * nt;
+                        dma16(k * 64 + x_piece < K / 8 ? xb + (size_t)t * K * 2 + k * 1024 + x_piece * 16 : zero, all_x + u * kXRow);
+                    }
                 stage_scales(gs + (size_t)n0 * blocks, my_s, K / 4, K % 64 == 0, 0, 1);
                 stage_scales(us + (size_t)n0 * blocks, my_s + K / 4, K / 4, K % 64 == 0, 0, 1);
             }
-            const bool load_x = at == (int)blockIdx.x || kc < K;
-            if (load_x) {
-                if (at != (int)blockIdx.x || k0 > 0) __syncthreads();           // the last chunk has been read
-                const int per_row = kc / 512;
-#pragma unroll 1
-                for (int i = wave; i < nt * per_row; i += nw) {
-                    const int t = i / per_row, c = (i - t * per_row) * 512 + lane * 8;
-                    dma16(c < kn ? reinterpret_cast<const char *>(x + (size_t)(t0 + t) * K + k0 + c) : reinterpret_cast<const char *>(g_zero16),
-                          lds + t * ldx * 2 + (i - t * per_row) * 1024);
-                }
-            }
             keep_order();
-            br = BranchLanes(bt);
-            u32x4 w[kRing + 1];
-            auto load = [&](int s) {                     // past the end the last one again
-                const int st = first + (s < steps ? s : steps - 1);
-                return ldg<u32x4>(codes + st * 64 + (st == all - 1 ? q_last : q * 16));
-            };
-#pragma unroll
-            for (int u = 0; u < kRing; ++u) w[u] = load(u);
-            if (load_x)
-                pipeline_barrier<kRing>();
-            else
-                wait_loads<kRing>();
-            asm volatile("" : "+v"(br.v_next), "+v"(br.v_alpha));      // arrived by now: not asked for at the end
+        }
+        const char *mine = lds;
+        char *fill = lds + AHEAD * stage;
+        f32x4 acc = {0, 0, 0, 0};
+        if (kWhole && at == (int)blockIdx.x) pipeline_barrier<(AHEAD - 1) * PER>();
 #pragma unroll 1
-            for (int s = 0; s < steps; s += kRing + 1) {
+        for (int c = 0; c < chunks; ++c) {
+            if (kWhole)
+                wait_loads<(AHEAD - 1) * PER>();
+            else
+                pipeline_barrier<(AHEAD - 1) * PER>();
+            issue(c + AHEAD, fill);
+            const char *mx = kWhole ? all_x + c * nt * kXRow : mine;
+            const char *sc = my_s + r16 * blocks + c * 16 + q * 4;
+            if (have)
 #pragma unroll
-                for (int u = 0; u < kRing + 1; ++u) {
-                    w[(u + kRing) % (kRing + 1)] = load(s + u + kRing);
-                    if (s + u >= steps) continue;        // no way out of the loop here: loads in flight are counted through it
-                    const int b = (first + s + u) * 4;
-                    const uint32_t byte = *reinterpret_cast<const uint8_t *>(sc + b);
-                    const float scale = scale_of(b + q < blocks ? byte : 127u);      // past the end x is zero
+            for (int s = 0; s < 4; ++s) {
+                const uint32_t byte = *reinterpret_cast<const uint8_t *>(sc + s);
+                const float scale = scale_of(c * 16 + q * 4 + s < blocks ? byte : 127u);
+                const u32x4 w = *reinterpret_cast<const u32x4 *>(mine + cb + r16 * 256 + ((q * 4 + s) ^ r16) * 16);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            widen8(w[u][j], scale), *reinterpret_cast<const bf16x8 *>(xr + (s + u) * 256 + j * 16), acc, 0, 0, 0);
-                }
+                for (int j = 0; j < 4; ++j)
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        widen8(w[j], scale), *reinterpret_cast<const bf16x8 *>(mx + xr + s * 256 + j * 16), acc, 0, 0, 0);
             }
+            mine = mine + stage == lds + S * stage ? lds : mine + stage;
+            fill = fill + stage == lds + S * stage ? lds : fill + stage;
         }
         if (!have) continue;
         // neurons 4q .. 4q + 3 of token r16: gate in groups q < 2, up in the lanes 32 on
         f32x4 up;
 #pragma unroll
         for (int i = 0; i < 4; ++i) up[i] = __shfl_xor(acc[i], 32);
+        const BranchLanes br(bt);
         gated<8, 1>(
             br, bt, n0, n0 + 4 * (q & 1), [&](int, int e, float &g, float &u) { g = acc[e], u = up[e]; },
             [&](int, int b) { return kOneRun || !route || (r16 < nt && route[(size_t)(t0 + r16) * bt.B + b] != 0); },
@@ -143,6 +166,7 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int K, int kc, const uint8_t *
                 if (q < 2 && r16 < nt) *reinterpret_cast<uint2 *>(H + (size_t)(t0 + r16) * ldh + h_place(n0 + 4 * q)) = h;
             });
     }
+    pipeline_barrier<0>();                               // loads past the end are still on their way into LDS
 }
 
 // Bytes of LDS of w4_down: S stages of nt tokens' H and of codes, a kilobyte that loads without a token fill, the scales, and
@@ -174,12 +198,11 @@ w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__
     char *scrap = lds + S * stage, *scales = scrap + 1024;
     uint32_t *bits = reinterpret_cast<uint32_t *>(scales + scale_bytes(K));
     uint16_t *list = reinterpret_cast<uint16_t *>(bits + (blocks + 31) / 32);
-    stage_scales(ds + (size_t)m0 * blocks, scales, K / 2, true, wave, W);
     const int s_beg = kOneRun ? run.beg / kStepK : 0;
     int steps = kOneRun ? (run.end + kStepK - 1) / kStepK - s_beg : 0;
     if constexpr (!kOneRun) {
-        __shared__ Shared sh;
-        mark_blocks(sh, bt.B, load_table(sh, bt, route, t0, nt), bits, blocks);
+        const OffsetLanes off(bt);
+        mark_blocks(off, live_of_16(bt, route, t0, nt), bits, blocks);
         // every wave counts the live steps, and together they write the list
 #pragma unroll 1
         for (int s = 0; s < all; s += 64) {
@@ -213,7 +236,11 @@ w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__
     const int chunks = (steps + W - 1) / W;
     keep_order();
 #pragma unroll 1
-    for (int c = 0; c < AHEAD; ++c) issue(c, lds + c * stage);
+    for (int c = 0; c < AHEAD; ++c) {
+        issue(c, lds + c * stage);
+        if (c == 0) stage_scales(ds + (size_t)m0 * blocks, scales, K / 2, true, wave, W);
+        keep_order();
+    }
     f32x4 acc = {0, 0, 0, 0};
     const char *mine = lds, *end = lds + S * stage;
     char *fill = lds + AHEAD * stage;
@@ -327,8 +354,6 @@ unsigned convert_blocks(size_t pieces)
     return (unsigned)(want < 8192 ? want : 8192);
 }
 
-size_t gate_up_lds(int nt, int nw, int kc, int K) { return (size_t)nt * (kc + kPad) * 2 + (size_t)nw * scale_bytes(K); }
-
 template <bool kOneRun, int W, int NL, int S>
 hipError_t launch_down(const W4Args &a, const BranchTable &bt, const Range &run)
 {
@@ -342,16 +367,52 @@ hipError_t launch_down(const W4Args &a, const BranchTable &bt, const Range &run)
     return launch_status("w4_down launch");
 }
 
+template <bool kOneRun, int XL, int S>
+hipError_t launch_gate_up(const W4Args &a, const BranchTable &bt, const Range &run, int groups, int nw, int tt)
+{
+    const size_t lds = gate_up_lds(a.T < tt ? a.T : tt, nw, S, a.d_model, XL == 0);
+    const hipError_t e = allow_lds<w4_gate_up<kOneRun, XL, S>>((int)lds, "w4_gate_up attribute");
+    if (e != hipSuccess) return e;
+    const int resident = 256 * (int)(160 * 1024 / lds);
+    const int grid = ceil_div(groups, nw) < resident ? ceil_div(groups, nw) : resident;
+    ProfileScope ps(MLPMOE_KERNEL_W4_GATE_UP, a.stream);
+    w4_gate_up<kOneRun, XL, S><<<dim3(grid, ceil_div(a.T, tt)), nw * 64, lds, a.stream>>>(
+        static_cast<const uint16_t *>(a.x), a.T, tt, a.d_model, a.gc, a.gs, a.uc, a.us, static_cast<uint16_t *>(a.H), a.ldh, a.route, run, bt);
+    return launch_status("w4_gate_up launch");
+}
+
+// A wave a group for every CU's share of the groups, up to 8; three stages, x whole if there is room for it.  (More stages, that
+// is requests in flight, take longer: 4096 x 14336, T = 1: four 18.0 us, three 16.8.)  Where three stages with x in them do not fit,
+// up to two waves fewer, then two stages.  A wave loads up to four tokens of x.
+template <bool kOneRun>
+hipError_t gate_up(const W4Args &a, const BranchTable &bt, const Range &run, int groups)
+{
+    const int nt = a.T < 16 ? a.T : 16, K = a.d_model, least = ceil_div(nt, 4);
+    auto fits = [&](int nw, int S, bool whole) { return gate_up_lds(nt, nw, S, K, whole) <= (size_t)kLdsBytes; };
+    int want = ceil_div(groups, 256);
+    want = want > 8 ? 8 : want;
+    if (fits(want, 3, true)) return launch_gate_up<kOneRun, 0, 3>(a, bt, run, groups, want, 16);
+    want = want < least ? least : want;
+    for (int n = want; n >= least && n >= want - 2; --n) {
+        if (!fits(n, 3, false)) continue;
+        const int xl = ceil_div(nt, n);
+        return xl <= 2   ? launch_gate_up<kOneRun, 2, 3>(a, bt, run, groups, n, 16)
+               : xl == 3 ? launch_gate_up<kOneRun, 3, 3>(a, bt, run, groups, n, 16)
+                         : launch_gate_up<kOneRun, 4, 3>(a, bt, run, groups, n, 16);
+    }
+    for (int n = want; n >= least; --n)
+        if (fits(n, 2, false)) return launch_gate_up<kOneRun, 4, 2>(a, bt, run, groups, n, 16);
+    return launch_gate_up<kOneRun, 4, 2>(a, bt, run, groups, 1, 4);      // scales of a very long K: one wave, four tokens at a time
+}
+
 // 16 waves while three stages of their chunks fit, else 8, whose chunks are half as long.
 template <bool kOneRun>
 hipError_t down(const W4Args &a, const BranchTable &bt, const Range &run)
 {
     const int nt = a.T < 16 ? a.T : 16, K = a.d_inter;
     auto fits = [&](int W, int S) { return down_lds(W, S, nt, K, kOneRun) <= (size_t)kLdsBytes; };
-    if (nt == 1 && fits(16, 7)) return launch_down<kOneRun, 16, 1, 7>(a, bt, run);
     if (nt <= 4 && fits(16, 4)) return launch_down<kOneRun, 16, 1, 4>(a, bt, run);
     if (nt <= 8 && fits(16, 3)) return launch_down<kOneRun, 16, 2, 3>(a, bt, run);
-    if (nt <= 12 && fits(8, 4)) return launch_down<kOneRun, 8, 3, 4>(a, bt, run);
     if (fits(8, 3)) return launch_down<kOneRun, 8, 4, 3>(a, bt, run);
     return launch_down<kOneRun, 8, 1, 3>(a, bt, run);    // scales of a very long K: four tokens at a time
 }
@@ -385,32 +446,14 @@ hipError_t launch_w4_dequantize(const uint8_t *codes, const uint8_t *scales, siz
 
 hipError_t launch_w4_forward(const W4Args &a, const BranchTable &bt)
 {
-    const int nt = a.T < 16 ? a.T : 16, token_tiles = ceil_div(a.T, 16), cus = 256;
     const bool one = !a.route && bt.n_runs == 1;
     const Range run = one ? Range{bt.run_start[0], bt.run_end[0]} : Range{0, 0};
     int groups = 0;                          // an upper bound: a group shared by two branches counts for both
     for (int b = 0; b < bt.B; ++b)
         if (((bt.active >> b) & 1) && bt.off[b + 1] > bt.off[b]) groups += ceil_div(bt.off[b + 1], 8) - bt.off[b] / 8;
     if (one) groups = ceil_div(run.end, 8) - run.beg / 8;
-    int nw = ceil_div(groups, cus);
-    if (nw > 8) nw = 8;
-    while (nw > 1 && gate_up_lds(nt, nw, 512, a.d_model) > (size_t)kLdsBytes) --nw;
-    int kc = ceil_div(a.d_model, 512) * 512;
-    while (gate_up_lds(nt, nw, kc, a.d_model) > (size_t)kLdsBytes) kc = ceil_div(kc / 2, 512) * 512;
-    const size_t lds = gate_up_lds(nt, nw, kc, a.d_model);
-    const int resident = cus * (lds > 78 * 1024 ? 1 : lds > 39 * 1024 ? 2 : 4);
-    int grid = ceil_div(groups, nw);
-    if (grid > resident) grid = resident;
-    hipError_t e = one ? allow_lds<w4_gate_up<true>>((int)lds, "w4_gate_up attribute") : allow_lds<w4_gate_up<false>>((int)lds, "w4_gate_up attribute");
+    const hipError_t e = one ? gate_up<true>(a, bt, run, groups) : gate_up<false>(a, bt, run, groups);
     if (e != hipSuccess) return e;
-    {
-        ProfileScope ps(MLPMOE_KERNEL_W4_GATE_UP, a.stream);
-        (one ? w4_gate_up<true> : w4_gate_up<false>)<<<dim3(grid, token_tiles), nw * 64, lds, a.stream>>>(
-            static_cast<const uint16_t *>(a.x), a.T, a.d_model, kc, a.gc, a.gs, a.uc, a.us, static_cast<uint16_t *>(a.H), a.ldh, a.route, run,
-            bt);
-        e = launch_status("w4_gate_up launch");
-        if (e != hipSuccess) return e;
-    }
     return one ? down<true>(a, bt, run) : down<false>(a, bt, run);
 }
 

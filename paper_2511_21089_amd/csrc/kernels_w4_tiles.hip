@@ -170,10 +170,11 @@ w4_tile_gate_up(const uint16_t *__restrict__ x, int T, int K, int d_inter, const
     if constexpr (kOneRun) {
         if (row == 0) clear_edges(run, H + (size_t)t0 * ldh, ldh, nt, wave, kWaves);
     } else {
-        __shared__ Shared sh;
-        const unsigned long long live = load_table(sh, bt, route, t0, nt);
-        groups = Groups<16, kOneRun>(sh, bt.B, live);
-        if (row == 0) clear_edges(sh, bt.B, live, H + (size_t)t0 * ldh, ldh, nt, wave, kWaves);
+        __shared__ unsigned any[2];
+        const OffsetLanes off(bt);
+        const unsigned long long live = live_of(bt, route, t0, nt, any);
+        groups = Groups<16, kOneRun>(off, live);
+        if (row == 0) clear_edges(off, bt.B, live, H + (size_t)t0 * ldh, ldh, nt, wave, kWaves);
         if (row * kWaves * NR >= groups.total) return;
     }
 
@@ -234,8 +235,9 @@ w4_tile_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_
     const int blocks = K / 32;
     uint32_t *bits = reinterpret_cast<uint32_t *>(lds + KW * core_lds(NA, NF, D));
     if constexpr (!kOneRun) {
-        __shared__ Shared sh;
-        mark_blocks(sh, bt.B, load_table(sh, bt, route, t0, nt), bits, blocks);
+        __shared__ unsigned any[2];
+        const OffsetLanes off(bt);
+        mark_blocks(off, live_of(bt, route, t0, nt, any), bits, blocks);
     }
     const int first = kOneRun ? run.beg / 32 : 0, last = kOneRun ? (run.end + 31) / 32 : blocks;      // live blocks lie here
     Rows rows[NA];

@@ -126,25 +126,49 @@ struct Range {
     int beg, end;
 };
 
-struct Shared {
-    int off[MLPMOE_MAX_BRANCHES + 1];
-    unsigned any[2];
+// Live branches of the tokens t0 .. t0 + nt - 1, looked through by the whole workgroup (any: two words of LDS).  Ends with a
+// barrier.
+__device__ __forceinline__ unsigned long long live_of(const BranchTable &bt, const uint8_t *route, int t0, int nt, unsigned *any)
+{
+    if (!route) return bt.active;
+    if (threadIdx.x < 2) any[threadIdx.x] = 0;
+    __syncthreads();
+    unsigned long long mine = 0;
+    int b = (int)threadIdx.x % bt.B;
+    const int add = (int)blockDim.x % bt.B;
+    for (int i = threadIdx.x; i < nt * bt.B; i += blockDim.x) {
+        if (route[(size_t)t0 * bt.B + i]) mine |= 1ULL << b;
+        b += add;
+        if (b >= bt.B) b -= bt.B;
+    }
+    if ((unsigned)mine) atomicOr(&any[0], (unsigned)mine);
+    if (mine >> 32) atomicOr(&any[1], (unsigned)(mine >> 32));
+    __syncthreads();
+    return (any[0] | ((unsigned long long)any[1] << 32)) & bt.active;
+}
+
+// Lane b of every wave: the offsets of branch b.
+struct OffsetLanes {
+    int beg, end;
+    __device__ __forceinline__ explicit OffsetLanes(const BranchTable &bt)
+    {
+        const int lane = threadIdx.x & 63;
+        beg = bt.off[lane];
+        end = bt.off[lane + 1];
+    }
+    __device__ __forceinline__ int first(int b) const { return __builtin_amdgcn_readlane(beg, b); }
+    __device__ __forceinline__ int past(int b) const { return __builtin_amdgcn_readlane(end, b); }
 };
 
-// Live branches of the tokens t0 .. t0 + nt - 1, and the offsets into LDS.  Ends with a barrier.
-__device__ __forceinline__ unsigned long long load_table(Shared &sh, const BranchTable &bt, const uint8_t *route, int t0, int nt)
+// Live branches of at most 16 tokens, every wave for itself: all routes asked for at once.
+__device__ __forceinline__ unsigned long long live_of_16(const BranchTable &bt, const uint8_t *route, int t0, int nt)
 {
-    const int tid = threadIdx.x;
-    if (tid < 2) sh.any[tid] = 0;
-    for (int i = tid; i <= MLPMOE_MAX_BRANCHES; i += blockDim.x) sh.off[i] = bt.off[i];
-    __syncthreads();
     if (!route) return bt.active;
-    for (int i = tid; i < nt * bt.B; i += blockDim.x) {
-        const int b = i % bt.B;
-        if (route[(size_t)t0 * bt.B + i]) atomicOr(&sh.any[b >> 5], 1u << (b & 31));
-    }
-    __syncthreads();
-    return (sh.any[0] | ((unsigned long long)sh.any[1] << 32)) & bt.active;
+    const int lane = threadIdx.x & 63, b = lane < bt.B ? lane : 0;
+    unsigned any = 0;
+#pragma unroll
+    for (int t = 0; t < 16; ++t) any |= route[(size_t)(t0 + (t < nt ? t : 0)) * bt.B + b];
+    return __ballot(any != 0 && lane < bt.B) & bt.active;
 }
 
 // The groups of G neurons, at multiples of G, that a live branch reaches into, numbered in order.
@@ -153,11 +177,11 @@ struct Groups {
     int beg, upto;           // lane b: first group that branch b adds to those of the live branches before it; their number with it
     int total;
     __device__ __forceinline__ Groups(const Range &run) : beg(run.beg / G), upto(0), total((run.end + G - 1) / G - run.beg / G) {}
-    __device__ __forceinline__ Groups(const Shared &sh, int B, unsigned long long live)
+    __device__ __forceinline__ Groups(const OffsetLanes &off, unsigned long long live)
     {
         const int lane = threadIdx.x & 63;
-        const bool on = lane < B && ((live >> lane) & 1);
-        const int lo = on ? sh.off[lane] : 0, hi = on ? sh.off[lane + 1] : 0;
+        const bool on = (live >> lane) & 1;
+        const int lo = on ? off.beg : 0, hi = on ? off.end : 0;
         int end = hi > lo ? (hi + G - 1) / G : 0;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -230,11 +254,11 @@ __device__ __forceinline__ void clear_edges(const Range &run, uint16_t *H, int l
     if (run.beg % kStepK) clear_range(H, ldh, nt, run.beg / kStepK * kStepK, run.beg, wave, nw);
     if (run.end % kStepK) clear_range(H, ldh, nt, run.end, (run.end + kStepK - 1) / kStepK * kStepK, wave, nw);
 }
-__device__ __forceinline__ void clear_edges(const Shared &sh, int B, unsigned long long live, uint16_t *H, int ldh, int nt, int wave,
-                                            int nw)
+__device__ __forceinline__ void clear_edges(const OffsetLanes &off, int B, unsigned long long live, uint16_t *H, int ldh, int nt,
+                                            int wave, int nw)
 {
     for (int b = 0; b <= B; ++b) {                       // past the last branch: the rest of its step
-        const int from = sh.off[b], to = b < B ? sh.off[b + 1] : ldh;
+        const int from = b < B ? off.first(b) : off.past(B - 1), to = b < B ? off.past(b) : ldh;
         if ((b < B && ((live >> b) & 1)) || to == from) continue;
         const int up = (from + kStepK - 1) / kStepK * kStepK, down = to / kStepK * kStepK;
         const int end = up < to ? up : to, beg = down > end ? down : end;
@@ -244,14 +268,20 @@ __device__ __forceinline__ void clear_edges(const Shared &sh, int B, unsigned lo
 }
 
 // A bit a block of the K axis of W_down: whether a live branch has a neuron in it.  Ends with a barrier.
-__device__ __forceinline__ void mark_blocks(const Shared &sh, int B, unsigned long long live, uint32_t *bits, int blocks)
+__device__ __forceinline__ void mark_blocks(const OffsetLanes &off, unsigned long long live, uint32_t *bits, int blocks)
 {
-    for (int i = threadIdx.x; i < (blocks + 31) / 32; i += blockDim.x) bits[i] = 0;
-    __syncthreads();
-    for (int b = 0; b < B; ++b) {
-        const int lo = sh.off[b], hi = sh.off[b + 1];
-        if (!((live >> b) & 1) || hi == lo) continue;
-        for (int i = lo / 32 + threadIdx.x; i <= (hi - 1) / 32; i += blockDim.x) atomicOr(&bits[i / 32], 1u << (i & 31));
+#pragma unroll 1
+    for (int i = threadIdx.x; i < (blocks + 31) / 32; i += blockDim.x) {
+        uint32_t w = 0;
+        for (unsigned long long m = live; m != 0; m &= m - 1) {
+            const int b = __builtin_ctzll(m), lo = off.first(b), hi = off.past(b);
+            // blocks lo / 32 .. (hi - 1) / 32 of this word's 32 i .. 32 i + 31
+            const int from = lo / 32 - 32 * i, to = (hi + 31) / 32 - 32 * i;
+            const uint32_t below = to <= 0 ? 0u : to >= 32 ? ~0u : (1u << to) - 1u;
+            const uint32_t less = from <= 0 ? 0u : from >= 32 ? ~0u : (1u << from) - 1u;
+            if (hi > lo) w |= below & ~less;
+        }
+        bits[i] = w;
     }
     __syncthreads();
 }
