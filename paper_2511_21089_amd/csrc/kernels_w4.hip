@@ -159,10 +159,10 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
 #pragma unroll
         for (int i = 0; i < 4; ++i) up[i] = __shfl_xor(acc[i], 32);
         const BranchLanes br(bt);
-        gated<8, 1>(
-            br, bt, n0, n0 + 4 * (q & 1), [&](int, int e, float &g, float &u) { g = acc[e], u = up[e]; },
-            [&](int, int b) { return kOneRun || !route || (r16 < nt && route[(size_t)(t0 + r16) * bt.B + b] != 0); },
-            [&](int, uint2 h) {
+        gated<8>(
+            br, bt, n0, n0 + 4 * (q & 1), acc, up,
+            [&](int b) { return kOneRun || !route || (r16 < nt && route[(size_t)(t0 + r16) * bt.B + b] != 0); },
+            [&](uint2 h) {
                 if (q < 2 && r16 < nt) *reinterpret_cast<uint2 *>(H + (size_t)(t0 + r16) * ldh + h_place(n0 + 4 * q)) = h;
             });
     }
@@ -203,16 +203,7 @@ w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__
     if constexpr (!kOneRun) {
         const OffsetLanes off(bt);
         mark_blocks(off, live_of_16(bt, route, t0, nt), bits, blocks);
-        // every wave counts the live steps, and together they write the list
-#pragma unroll 1
-        for (int s = 0; s < all; s += 64) {
-            const int st = s + lane;
-            const bool on = st < all && ((bits[st / 8] >> (st % 8 * 4)) & 15u) != 0;
-            const unsigned long long m = __ballot(on);
-            if (on) list[steps + __popcll(m & ((1ULL << lane) - 1))] = (uint16_t)st;
-            steps += __popcll(m);
-        }
-        __syncthreads();
+        steps = list_steps(bits, all, list);
     }
     const uint8_t *codes = dc + (size_t)(m0 + r16) * (K / 2);
     const char *hb = reinterpret_cast<const char *>(H + (size_t)t0 * ldh);

@@ -1,302 +1,317 @@
 // The forward on 4-bit weights for more tokens than one MFMA column block: tiles of rows x tokens.
 //
-// A workgroup of four waves owns 16 NF tokens and 16 NA rows of weights a wave.  The tokens' x (or H) goes through LDS, shared
-// by the waves, 128 of K at a time and D steps ahead, loaded straight into LDS; each wave loads the codes of its own rows
-// straight into registers, 16 bytes a lane = one block of 32, also D steps ahead, and widens them there: a weight is widened
-// once for 16 NF tokens, half an instruction a weight against NF MFMA columns.  LDS holds a token's 128 values as 16 pieces of
-// 16 bytes, piece c at place c ^ (token mod 16), so that the lanes of a cycle read different banks.
+// A workgroup owns 16 NF tokens and, for each of its WR row waves, 16 NA rows of weights.  x (or H) goes through LDS, shared by the
+// waves; each wave's codes go through LDS too, read back by the lanes that loaded them, and are widened in registers: a weight
+// is widened once for 16 NF tokens, half an instruction a weight against NF MFMA columns.  K goes by steps of 128, AHEAD stages
+// of KW steps ahead; with KW = 2 two sets of row waves take the steps in turn and add their sums at the end, which gives a tile
+// that is too small for two workgroups on a CU two waves a SIMD.  LDS holds a token's 128 values as 16 pieces of 16 bytes, piece c
+// at place c ^ (token mod 16), so that the lanes of a cycle read different banks.
 //
 // Rows are the MFMA's rows and tokens its columns: a lane ends with four neighbouring neurons (features) of a token, one store.
+// Nothing is loaded into registers: beside loads into LDS the compiler waits for every register load at once.
 #include "w4_common.h"
 
 namespace mlpmoe {
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kScaleLd = 80;             // bytes of LDS for the scales of 2048 of K of a row: 64, and 16 for other banks
+constexpr int kScaleBuf = 1280;          // scales of a wave's rows for 512 of K: 16 bytes a row, or 20 in five loads of a dword
 
-// One set of four waves: the ring of x or H, and the scales of its rows.
-constexpr int core_lds(int NA, int NF, int D) { return (D + 1) * NF * 4096 + kWaves * NA * 16 * kScaleLd; }
-
-// The codes and scales of 16 rows.
-struct Rows {
-    __amdgpu_buffer_rsrc_t codes;
-    const uint8_t *scales, *end;             // of these rows, of the matrix
-    __device__ __forceinline__ void set(const uint8_t *c, const uint8_t *s, int row, int all_rows, int K)
-    {
-        end = s + (size_t)all_rows * (K / 32);
-        codes = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(c + (size_t)row * (K / 2)), 0, 16u * (unsigned)(K / 2),
-                                                 0x00027000);
-        scales = s + (size_t)row * (K / 32);
-    }
-};
-
-// acc[a][f] += rows a x tokens f over steps of K.  KW sets of four waves share the steps out: next() names KW at a time (the first
-// of them, or -1: no more) and set kw takes the first + kw unless that is past the end or not live; live(s): the blocks of step
-// s to be read, four bits, 0 past the end.  The sum is in the first set's waves.  kPlaced: X is H, whose pieces lie in the
-// order in which they are read.
-template <int NA, int NF, int D, int KW, bool kPlaced, typename Next, typename Live>
-__device__ __forceinline__ void sum_steps(f32x4 (&acc)[NA][NF], const Rows (&rows)[NA], const uint16_t *__restrict__ X, int ldx,
-                                          int last_token, int K, char *lds, Next next, Live live)
+constexpr int stage_bytes(int NA, int NF, int KW, int WR) { return KW * NF * 4096 + KW * WR * NA * 1024; }
+constexpr int core_lds(int NA, int NF, int AHEAD, int KW, int WR)
 {
-    constexpr int R = D + 1, STAGE = NF * 16 * 256, PER = NF + NA;
-    static_assert((D - 1) * PER < 63, "the counter of loads in flight holds six bits");
-    const int lane = threadIdx.x & 63, r16 = lane & 15, q = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kWaves;
-    const int kw = KW > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kWaves : 0;
-    char *all_lds = lds;
-    lds += kw * core_lds(NA, NF, D);
-    // this lane's part of the loads into LDS: four tokens a load, 16 pieces each
-    unsigned x_off[NF], x_blk[NF];
-#pragma unroll
-    for (int n = 0; n < NF; ++n) {
-        const int t = (wave * NF + n) * 4 + q;
-        const unsigned c = (unsigned)(r16 ^ (t & 15));
-        x_off[n] = (unsigned)(t < last_token ? t : last_token) * (unsigned)ldx * 2u + (kPlaced ? (c & 3) * 4 + c / 4 : c) * 16u;
-        x_blk[n] = c / 4;
-    }
-    const unsigned w_off = (unsigned)r16 * (unsigned)(K / 2) + (unsigned)q * 16u;
-    const char *xb = reinterpret_cast<const char *>(X), *zero = reinterpret_cast<const char *>(g_zero16);
+    return (AHEAD + 1) * (stage_bytes(NA, NF, KW, WR) + KW * WR * kScaleBuf);
+}
 
-    u32x4 w[R][NA];
-    int step[R];
-    bool on[R];                             // this lane's block of the step
-    auto issue = [&](int s, int slot) {
-        const unsigned ok = s < 0 ? 0u : live(s + kw);
-        char *dst = lds + slot * STAGE + wave * (NF * 1024);
-        const char *src = xb + (size_t)(s < 0 ? 0 : s + kw) * 256;
+// acc[a][f] += 16 rows (codes[a], this wave's) x 16 tokens over the n > 0 steps step(0) .. step(n - 1), ascending (past the end
+// the last one).  srow:
+// this lane's row of scales, lane 16 a + r for row r of codes[a]; send: their end.  on(b): whether block b is read (the scale of
+// another may be no number; x is zero there).  The sum is in the first set's waves.  kPlaced: X is H, whose pieces lie in the
+// order in which they are read, rows of whole steps; else a row is K long.
+template <int NA, int NF, int AHEAD, int KW, int WR, bool kPlaced, typename StepOf, typename On>
+__device__ __forceinline__ void sum_steps(f32x4 (&acc)[NA][NF], const uint8_t *const (&codes)[NA], const uint8_t *srow,
+                                          const uint8_t *send, const uint16_t *__restrict__ X, int ldx, int last_token, int K,
+                                          char *lds, int n, StepOf step_of, On on)
+{
+    constexpr int STAGE = stage_bytes(NA, NF, KW, WR), NX = NF * 4 / WR, PER = NX + NA;
+    static_assert(NF * 4 % WR == 0 && (AHEAD - 1) * PER < 63 && NA <= 4, "loads in flight");
+    const int lane = threadIdx.x & 63, r16 = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kw = wave / WR;
+    const int blocks = K / 32, all = (K + kStepK - 1) / kStepK;
+    const char *xb = reinterpret_cast<const char *>(X), *zero = reinterpret_cast<const char *>(g_zero16);
+    // this lane's part of the loads of X: four tokens a load, 16 pieces each
+    unsigned x_off[NX];
+    int x_k[NX];
 #pragma unroll
-        for (int n = 0; n < NF; ++n) dma16((ok >> x_blk[n]) & 1u ? src + x_off[n] : zero, dst + n * 1024);
-        on[slot] = (ok >> q) & 1u;
-        const unsigned wo = on[slot] ? w_off + (unsigned)(s + kw) * 64u : 0xffffffffu;
+    for (int i = 0; i < NX; ++i) {
+        const int unit = wave * NX + i, t = unit % (NF * 4) * 4 + q, c = r16 ^ (t & 15);
+        x_off[i] = (unsigned)((t < last_token ? t : last_token) * ldx * 2 + (kPlaced ? (c & 3) * 4 + c / 4 : c) * 16);
+        x_k[i] = c * 8;
+    }
+    const int w_row = r16 * (K / 2);
+    const int q_last = q < blocks - (all - 1) * 4 ? q : 0;              // in the last step there may be fewer blocks than groups of lanes
+    const bool by16 = K % 512 == 0;
+    const int late = by16 ? 0 : (r16 * blocks) & 3;                     // bytes of a dword before a row's
+    char *my_s = lds + (AHEAD + 1) * STAGE + wave * ((AHEAD + 1) * kScaleBuf);
+    const int w_at = KW * NF * 4096 + wave * (NA * 1024);
+    int have = -1, slot = 0;                                            // the last 512 of K whose scales were asked for, and where
+    auto issue = [&](int i, char *dst) {                                // stage i: steps KW i ..; always PER loads, and at times scales
+        const int s = step_of(i * KW + kw);                             // past the end the last one again
+        if (s / 4 != have) {
+            have = s / 4;
+            slot = slot == AHEAD ? 0 : slot + 1;
+            char *to = my_s + slot * kScaleBuf;
+            if (by16) {
+                dma16(srow + have * 16, to);
+            } else {
+                const uint8_t *p = reinterpret_cast<const uint8_t *>(reinterpret_cast<uintptr_t>(srow + have * 16) & ~(uintptr_t)3);
+#pragma unroll 1
+                for (int d = 0; d < 5; ++d)
+                    __builtin_amdgcn_global_load_lds((gptr_t)(p + d * 4 < send ? p + d * 4 : p), (lptr_t)(to + d * 256), 4, 0, 0);
+            }
+        }
 #pragma unroll
-        for (int a = 0; a < NA; ++a) w[slot][a] = __builtin_amdgcn_raw_buffer_load_b128(rows[a].codes, wo, 0, 0);
-        step[slot] = s;
+        for (int j = 0; j < NX; ++j) {
+            const int u = KW == 1 ? s : step_of(i * KW + (wave * NX + j) / (NF * 4));
+            const char *src = xb + (size_t)u * 256 + x_off[j];
+            if (!kPlaced && u == all - 1) src = u * kStepK + x_k[j] < K ? src : zero;
+            dma16(src, dst + (wave * NX + j) * 1024);
+        }
+        const int off = w_row + s * 64 + (s == all - 1 ? q_last : q) * 16;
+#pragma unroll
+        for (int a = 0; a < NA; ++a) dma16(codes[a] + off, dst + w_at + a * 1024);
     };
-    // scales: 16 steps' worth of this wave's rows at a time, four lanes a row
-    char *my_s = lds + R * STAGE + wave * (NA * 16 * kScaleLd);
-    const int s_row = lane >> 2, s_piece = (lane & 3) * 16;
-    ScalePiece ahead[NA];
-    int chunk = -1, ahead_of = -1;
-    auto load_scales = [&](int c) {
-#pragma unroll
-        for (int a = 0; a < NA; ++a) ahead[a].load(rows[a].scales + (size_t)s_row * (K / 32) + c * 64 + s_piece, rows[a].end);
-        ahead_of = c;
-    };
-#pragma unroll
-    for (int u = 0; u < D; ++u) {
-        issue(next(), u);
+    const int stages = (n + KW - 1) / KW;
+    keep_order();
+#pragma unroll 1
+    for (int i = 0; i < AHEAD; ++i) {
+        issue(i, lds + i * STAGE);
         keep_order();
     }
-    for (bool more = true; more;) {
+    char *mine = lds, *fill = lds + AHEAD * STAGE;
+    int read = -1, rslot = 0;
+    const int a_step = by16 ? 256 : 64;
+#pragma unroll 1
+    for (int i = 0; i < stages; ++i) {
+        pipeline_barrier<(AHEAD - 1) * PER>();
+        const int s = step_of(i * KW + kw);
+        if (s / 4 != read) read = s / 4, rslot = rslot == AHEAD ? 0 : rslot + 1;
+        const int at = late + s % 4 * 4 + q;
+        const char *sc = my_s + rslot * kScaleBuf + (by16 ? r16 * 16 + at : (at >> 2) * 256 + r16 * 4 + (at & 3));
+        const char *st = mine + kw * (NF * 4096) + r16 * 256;
+        const bool live = on(s * 4 + q), mine_too = KW == 1 || i * KW + kw < n;
+        float scale[NA];
+        u32x4 w[NA];
+        bf16x8 xv[2][NF];
+        auto read_x = [&](int j) {
 #pragma unroll
-        for (int u = 0; u < R; ++u) {
-            if (step[u] < 0) {
-                more = false;
-                break;
-            }
-            const int s = step[u] + kw;
-            if (s / 16 != chunk) {
-                chunk = s / 16;
-                if (ahead_of != chunk) load_scales(chunk);
+            for (int f = 0; f < NF; ++f) xv[j & 1][f] = *reinterpret_cast<const bf16x8 *>(st + f * 4096 + (((q * 4 + j) ^ r16) * 16));
+        };
 #pragma unroll
-                for (int a = 0; a < NA; ++a) ahead[a].place(my_s + (a * 16 + s_row) * kScaleLd + s_piece);
-                if ((chunk + 1) * 64 < K / 32) load_scales(chunk + 1);
-            }
-            pipeline_barrier<(D - 1) * PER>();
-            issue(next(), (u + D) % R);
-            const char *st = lds + u * STAGE + r16 * 256;
-            float scale[NA];
+        for (int a = 0; a < NA; ++a) {
+            const uint32_t byte = *reinterpret_cast<const uint8_t *>(sc + a * a_step);
+            w[a] = *reinterpret_cast<const u32x4 *>(mine + w_at + a * 1024 + lane * 16);
+            // the second set has no step where their number is odd: codes of zero
+            if (KW > 1 && !mine_too) w[a] = u32x4{0, 0, 0, 0};
+            scale[a] = scale_of(live && mine_too ? byte : 127u);
+        }
+        read_x(0);
+        // The compiler waits for all reads of LDS at the first use of one, so the next reads come after the first products.
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
 #pragma unroll
             for (int a = 0; a < NA; ++a) {
-                scale[a] = scale_of(*reinterpret_cast<const uint8_t *>(my_s + (a * 16 + r16) * kScaleLd + s % 16 * 4 + q));
-                scale[a] = on[u] ? scale[a] : 1.0f;      // that of a block that is not read may be no number
-            }
+                const bf16x8 wv = widen8(w[a][j], scale[a]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                bf16x8 wv[NA];
-#pragma unroll
-                for (int a = 0; a < NA; ++a) wv[a] = widen8(w[u][a][j], scale[a]);
-#pragma unroll
-                for (int f = 0; f < NF; ++f) {
-                    const bf16x8 xv = *reinterpret_cast<const bf16x8 *>(st + f * (16 * 256) + (((q * 4 + j) ^ r16) * 16));
-#pragma unroll
-                    for (int a = 0; a < NA; ++a) acc[a][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[a], xv, acc[a][f], 0, 0, 0);
+                for (int f = 0; f < NF; ++f) acc[a][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[j & 1][f], acc[a][f], 0, 0, 0);
+                if (a == 0) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (j == 0) issue(i + AHEAD, fill);
+                    if (j < 3) read_x(j + 1);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
+        mine = mine + STAGE == lds + (AHEAD + 1) * STAGE ? lds : mine + STAGE;
+        fill = fill + STAGE == lds + (AHEAD + 1) * STAGE ? lds : fill + STAGE;
     }
-    pipeline_barrier<0>();                  // what is still on its way into LDS is zeros; let it land
+    pipeline_barrier<0>();                  // what is still on its way into LDS
     if constexpr (KW > 1) {
-        static_assert(KW == 2 && kWaves * NA * NF * 1024 <= KW * core_lds(NA, NF, D), "the second set's sums fit where the rings were");
-        f32x4 *s = reinterpret_cast<f32x4 *>(all_lds) + wave * (NA * NF * 64) + lane;
+        static_assert(KW == 2 && WR * NA * NF * 1024 <= (AHEAD + 1) * STAGE, "the second set's sums fit where the stages were");
+        f32x4 *sums = reinterpret_cast<f32x4 *>(lds) + (wave % WR) * (NA * NF * 64) + lane;
         if (kw == 1) {
 #pragma unroll
-            for (int i = 0; i < NA * NF; ++i) s[i * 64] = acc[i / NF][i % NF];
+            for (int i = 0; i < NA * NF; ++i) sums[i * 64] = acc[i / NF][i % NF];
         }
         pipeline_barrier<0>();
         if (kw == 0) {
 #pragma unroll
-            for (int i = 0; i < NA * NF; ++i) acc[i / NF][i % NF] += s[i * 64];
+            for (int i = 0; i < NA * NF; ++i) acc[i / NF][i % NF] += sums[i * 64];
         }
+        pipeline_barrier<0>();              // LDS is free again
     }
 }
 
-// Workgroup ids to tiles: the token tiles of a row tile on one XCD, one after the other, since they read the same weights.
-// Returns false past the last tile.  grid = 8 * ceil(row_tiles / 8) * token_tiles.
-__device__ __forceinline__ bool tile_of(int id, int row_tiles, int token_tiles, int &row, int &token)
+// Calls fn(f, sum) for f = 0 .. NF - 1, sum(a) this lane's acc[a][f], in a loop that is not unrolled, through BYTES of LDS of this
+// wave's own: an epilogue that is written out for every sum is thousands of instructions that run once.
+template <int NA, int NF, int BYTES, typename Fn>
+__device__ __forceinline__ void each_sum(const f32x4 (&acc)[NA][NF], char *lds, Fn fn)
 {
-    const int xcd = id % 8, at = id / 8;
-    token = at % token_tiles;
-    row = at / token_tiles * 8 + xcd;
-    return row < row_tiles;
+    constexpr int F = NA * NF * 1024 <= BYTES ? NF : NA * ((NF + 1) / 2) * 1024 <= BYTES ? (NF + 1) / 2 : NF / 4;
+    static_assert(F > 0 && NA * F * 1024 <= BYTES, "room for the sums of some of the tokens");
+    f32x4 *mine = reinterpret_cast<f32x4 *>(lds) + (threadIdx.x & 63);
+#pragma unroll 1
+    for (int f0 = 0; f0 < NF; f0 += F) {
+#pragma unroll
+        for (int p = 0; p < NF; p += F)
+            if (f0 == p) {
+#pragma unroll
+                for (int a = 0; a < NA; ++a)
+#pragma unroll
+                    for (int f = 0; f < F; ++f)
+                        if (p + f < NF) mine[(a * F + f) * 64] = acc[a][p + f];
+            }
+#pragma unroll 1
+        for (int f = f0; f < f0 + F && f < NF; ++f) fn(f, [&](int a) { return mine[(a * F + f - f0) * 64]; });
+    }
 }
 
-// A wave takes NR groups of 16 neurons that a live branch reaches into, at multiples of 16.
-template <int NR, int NF, int D, int KW, int W, bool kOneRun>
-__global__ void __launch_bounds__(KW * kWaves * 64, W)
+// Grid (8, token tiles, row tiles / 8): workgroups go to the XCDs in turn, so the token tiles of a row tile, which read the same
+// weights, are on one XCD, one after the other.
+
+// A row wave takes NR groups of 16 neurons that a live branch reaches into, at multiples of 16: rows of W_gate, then of W_up.
+template <int NR, int NF, int AHEAD, int KW, int WR, int W, bool kOneRun>
+__global__ void __launch_bounds__(KW * WR * 64, W)
 w4_tile_gate_up(const uint16_t *__restrict__ x, int T, int K, int d_inter, const uint8_t *__restrict__ gc, const uint8_t *__restrict__ gs,
                 const uint8_t *__restrict__ uc, const uint8_t *__restrict__ us, uint16_t *__restrict__ H, int ldh,
-                const uint8_t *__restrict__ route, int row_tiles, int token_tiles, Range run, BranchTable bt)
+                const uint8_t *__restrict__ route, int row_tiles, Range run, BranchTable bt)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int row, token;
-    if (!tile_of(blockIdx.x, row_tiles, token_tiles, row, token)) return;
-    const int t0 = token * 16 * NF, nt = T - t0 < 16 * NF ? T - t0 : 16 * NF;
+    const int row = blockIdx.z * 8 + blockIdx.x;
+    if (row >= row_tiles) return;
+    const int t0 = blockIdx.y * 16 * NF, nt = T - t0 < 16 * NF ? T - t0 : 16 * NF;
     const int lane = threadIdx.x & 63, r16 = lane & 15, q = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kWaves;
-    BranchLanes br(bt);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WR;
     Groups<16, kOneRun> groups(run);
     if constexpr (kOneRun) {
-        if (row == 0) clear_edges(run, H + (size_t)t0 * ldh, ldh, nt, wave, kWaves);
+        if (row == 0) clear_edges(run, H + (size_t)t0 * ldh, ldh, nt, wave, WR);
     } else {
         __shared__ unsigned any[2];
         const OffsetLanes off(bt);
         const unsigned long long live = live_of(bt, route, t0, nt, any);
         groups = Groups<16, kOneRun>(off, live);
-        if (row == 0) clear_edges(off, bt.B, live, H + (size_t)t0 * ldh, ldh, nt, wave, kWaves);
-        if (row * kWaves * NR >= groups.total) return;
+        if (row == 0) clear_edges(off, bt.B, live, H + (size_t)t0 * ldh, ldh, nt, wave, WR);
+        if (row * WR * NR >= groups.total) return;
     }
 
-    int group[NR];
-    Rows rows[2 * NR];
+    const int blocks = K / 32;
+    const uint8_t *codes[2 * NR], *srow = gs;
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
-        const int idx = (row * kWaves + wave) * NR + i;
-        group[i] = groups(idx < groups.total ? idx : groups.total - 1);
-        rows[i].set(gc, gs, group[i] * 16, d_inter, K);
-        rows[NR + i].set(uc, us, group[i] * 16, d_inter, K);
-        if (idx >= groups.total) group[i] = -1;
+        const int idx = (row * WR + wave) * NR + i;
+        const int g = groups(idx < groups.total ? idx : groups.total - 1);
+        codes[i] = gc + (size_t)g * 16 * (K / 2);
+        codes[NR + i] = uc + (size_t)g * 16 * (K / 2);
+        const size_t at = (size_t)(g * 16 + r16) * blocks;
+        if (q == i) srow = gs + at;
+        if (q == NR + i) srow = us + at;
     }
     f32x4 acc[2 * NR][NF];
 #pragma unroll
     for (int a = 0; a < 2 * NR; ++a)
 #pragma unroll
         for (int f = 0; f < NF; ++f) acc[a][f] = f32x4{0, 0, 0, 0};
-    const int steps = (K + kStepK - 1) / kStepK, blocks = K / 32;
-    int at = -KW;
-    sum_steps<2 * NR, NF, D, KW, false>(
-        acc, rows, x + (size_t)t0 * K, K, nt - 1, K, lds, [&]() { return (at += KW) < steps ? at : -1; },
-        [&](int s) { return blocks - s * 4 >= 4 ? 15u : blocks - s * 4 <= 0 ? 0u : (1u << (blocks - s * 4)) - 1u; });
-    if (KW > 1 && threadIdx.x >= kWaves * 64) return;
+    const int steps = (K + kStepK - 1) / kStepK;
+    sum_steps<2 * NR, NF, AHEAD, KW, WR, false>(
+        acc, codes, srow, (q < NR || q >= 2 * NR ? gs : us) + (size_t)d_inter * blocks, x + (size_t)t0 * K, K, nt - 1, K, lds, steps,
+        [&](int i) { return i < steps ? i : steps - 1; }, [&](int b) { return b < blocks; });
+    if (KW > 1 && threadIdx.x >= WR * 64) return;
 
-#pragma unroll
-    for (int i = 0; i < NR; ++i) {
-        if (group[i] < 0) continue;
-        const int n0 = group[i] * 16;
-        gated<16, NF>(
-            br, bt, n0, n0 + 4 * q, [&](int f, int e, float &g, float &u) { g = acc[i][f][e], u = acc[NR + i][f][e]; },
-            [&](int f, int b) {
-                const int t = f * 16 + r16;
-                return kOneRun || !route || (t < nt && route[(size_t)(t0 + t) * bt.B + b] != 0);
-            },
-            [&](int f, uint2 h) {
-                const int t = f * 16 + r16;
-                if (t < nt) *reinterpret_cast<uint2 *>(H + (size_t)(t0 + t) * ldh + h_place(n0 + 4 * q)) = h;
-            });
-    }
+    const BranchLanes br(bt);
+    constexpr int MINE = (AHEAD + 1) * stage_bytes(2 * NR, NF, KW, WR) / WR / 1024 * 1024;
+    each_sum<2 * NR, NF, MINE>(acc, lds + wave * MINE, [&](int f, auto sum) {
+        const int t = f * 16 + r16;
+#pragma unroll 1
+        for (int i = 0; i < NR; ++i) {
+            const int idx = (row * WR + wave) * NR + i;
+            if (idx >= groups.total) break;
+            const int n0 = groups(idx) * 16;
+            const f32x4 g = sum(i), u = sum(NR + i);
+            gated<16>(
+                br, bt, n0, n0 + 4 * q, g, u,
+                [&](int b) { return kOneRun || !route || (t < nt && route[(size_t)(t0 + t) * bt.B + b] != 0); },
+                [&](uint2 h) {
+                    if (t < nt) *reinterpret_cast<uint2 *>(H + (size_t)(t0 + t) * ldh + h_place(n0 + 4 * q)) = h;
+                });
+        }
+    });
 }
 
-// K is cut into `splits` ranges; with more than one the sums go to partial [splits][T][d_model].
-template <int NA, int NF, int D, int KW, int W, bool kOneRun>
-__global__ void __launch_bounds__(KW * kWaves * 64, W)
+// K is cut into 2^log_splits ranges; with more than one the sums go to partial [ranges][T][d_model].
+template <int NA, int NF, int AHEAD, int KW, int WR, int W, bool kOneRun>
+__global__ void __launch_bounds__(KW * WR * 64, W)
 w4_tile_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__restrict__ dc, const uint8_t *__restrict__ ds,
-             int d_model, void *__restrict__ out, int out_bf16, float *__restrict__ partial, int splits,
-             const uint8_t *__restrict__ route, int row_tiles, int token_tiles, Range run, BranchTable bt)
+             int d_model, void *__restrict__ out, int out_bf16, float *__restrict__ partial, int log_splits,
+             const uint8_t *__restrict__ route, int row_tiles, Range run, BranchTable bt)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int row, token;
-    if (!tile_of(blockIdx.x, row_tiles * splits, token_tiles, row, token)) return;
-    const int z = row / row_tiles;
-    row -= z * row_tiles;
-    const int t0 = token * 16 * NF, nt = T - t0 < 16 * NF ? T - t0 : 16 * NF;
+    const int row = blockIdx.z * 8 + blockIdx.x, splits = 1 << log_splits;
+    if (row >= row_tiles) return;
+    const int z = blockIdx.y & (splits - 1);
+    const int t0 = (blockIdx.y >> log_splits) * 16 * NF, nt = T - t0 < 16 * NF ? T - t0 : 16 * NF;
     const int lane = threadIdx.x & 63, r16 = lane & 15, q = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kWaves;
-    const int blocks = K / 32;
-    uint32_t *bits = reinterpret_cast<uint32_t *>(lds + KW * core_lds(NA, NF, D));
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WR;
+    const int blocks = K / 32, all = (K + kStepK - 1) / kStepK;
+    uint32_t *bits = reinterpret_cast<uint32_t *>(lds + core_lds(NA, NF, AHEAD, KW, WR));
+    uint16_t *list = reinterpret_cast<uint16_t *>(bits + (blocks + 31) / 32);
+    const int s_beg = kOneRun ? run.beg / kStepK : 0;
+    int steps = kOneRun ? (run.end + kStepK - 1) / kStepK - s_beg : 0;
     if constexpr (!kOneRun) {
         __shared__ unsigned any[2];
         const OffsetLanes off(bt);
         mark_blocks(off, live_of(bt, route, t0, nt, any), bits, blocks);
+        steps = list_steps(bits, all, list);
     }
-    const int first = kOneRun ? run.beg / 32 : 0, last = kOneRun ? (run.end + 31) / 32 : blocks;      // live blocks lie here
-    Rows rows[NA];
-    int group[NA];
+    const uint8_t *codes[NA], *srow = ds;
 #pragma unroll
     for (int a = 0; a < NA; ++a) {
-        group[a] = (row * kWaves + wave) * NA + a;
-        rows[a].set(dc, ds, (group[a] * 16 < d_model ? group[a] * 16 : d_model - 16), d_model, K);
+        const int want = (row * WR + wave) * NA + a, g = want * 16 < d_model ? want : d_model / 16 - 1;
+        codes[a] = dc + (size_t)g * 16 * (K / 2);
+        if (q == a) srow = ds + (size_t)(g * 16 + r16) * blocks;
     }
     f32x4 acc[NA][NF];
 #pragma unroll
     for (int a = 0; a < NA; ++a)
 #pragma unroll
         for (int f = 0; f < NF; ++f) acc[a][f] = f32x4{0, 0, 0, 0};
-    const int s_beg = first / 4, steps = (last + 3) / 4 - s_beg;
-    const int end = s_beg + (int)((long long)steps * (z + 1) / splits);
-    int at = s_beg + (int)((long long)steps * z / splits) - KW;
-    auto live = [&](int s) -> unsigned {
-        if (s >= end) return 0u;
-        if (!kOneRun) return ((unsigned)__builtin_amdgcn_readfirstlane(bits[s / 8]) >> (s % 8 * 4)) & 15u;      // 0 past the last block
-        unsigned m = last - s * 4 >= 4 ? 15u : (1u << (last - s * 4)) - 1u;
-        if (first > s * 4) m &= ~((1u << (first - s * 4)) - 1u);
-        return m;
-    };
-    sum_steps<NA, NF, D, KW, true>(
-        acc, rows, H + (size_t)t0 * ldh, ldh, nt - 1, K, lds,
-        [&]() {
-            at += KW;
-            if (!kOneRun)
-                for (; at < end; at += KW) {
-                    unsigned any = 0;
-#pragma unroll
-                    for (int k = 0; k < KW; ++k) any |= live(at + k);
-                    if (any) break;
-                }
-            return at < end ? at : -1;
-        },
-        live);
-    if (KW > 1 && threadIdx.x >= kWaves * 64) return;
+    const int beg = steps * z >> log_splits, n = (steps * (z + 1) >> log_splits) - beg;
+    if (n > 0)
+        sum_steps<NA, NF, AHEAD, KW, WR, true>(
+            acc, codes, srow, ds + (size_t)d_model * blocks, H + (size_t)t0 * ldh, ldh, nt - 1, K, lds, n,
+            [&](int i) {
+                const int at = beg + (i < n ? i : n - 1);
+                return kOneRun ? s_beg + at : __builtin_amdgcn_readfirstlane((int)list[at]);
+            },
+            [&](int b) { return b < blocks && (kOneRun ? b >= run.beg / 32 && b * 32 < run.end : (bits[b / 32] >> (b & 31) & 1) != 0); });
+    if (KW > 1 && threadIdx.x >= WR * 64) return;
 
-#pragma unroll
-    for (int a = 0; a < NA; ++a) {
-        const int m = group[a] * 16 + 4 * q;
-        if (m >= d_model) continue;
-#pragma unroll
-        for (int f = 0; f < NF; ++f) {
-            const int t = f * 16 + r16;
-            if (t >= nt) continue;
+    constexpr int MINE = (AHEAD + 1) * stage_bytes(NA, NF, KW, WR) / WR / 1024 * 1024;
+    each_sum<NA, NF, MINE>(acc, lds + wave * MINE, [&](int f, auto sum) {
+        const int t = f * 16 + r16;
+#pragma unroll 1
+        for (int a = 0; a < NA; ++a) {
+            const int m = ((row * WR + wave) * NA + a) * 16 + 4 * q;
+            const f32x4 v = sum(a);
+            if (m >= d_model || t >= nt) continue;
             const size_t to = (size_t)(t0 + t) * d_model + m;
             if (splits > 1)
-                *reinterpret_cast<f32x4 *>(partial + (size_t)z * T * d_model + to) = acc[a][f];
+                *reinterpret_cast<f32x4 *>(partial + (size_t)z * T * d_model + to) = v;
             else if (out_bf16)
-                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + to) =
-                    uint2{(uint32_t)to_bf16(acc[a][f][0]) | (uint32_t)to_bf16(acc[a][f][1]) << 16,
-                          (uint32_t)to_bf16(acc[a][f][2]) | (uint32_t)to_bf16(acc[a][f][3]) << 16};
+                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + to) = uint2{(uint32_t)to_bf16(v[0]) | (uint32_t)to_bf16(v[1]) << 16,
+                                                                                      (uint32_t)to_bf16(v[2]) | (uint32_t)to_bf16(v[3]) << 16};
             else
-                *reinterpret_cast<f32x4 *>(static_cast<float *>(out) + to) = acc[a][f];
+                *reinterpret_cast<f32x4 *>(static_cast<float *>(out) + to) = v;
         }
-    }
+    });
 }
 
 // The partial sums of a split, in order.
@@ -316,7 +331,7 @@ w4_reduce(const float *__restrict__ partial, size_t n4, int splits, void *__rest
 
 Range run_of(const W4Args &a, const BranchTable &bt) { return !a.route && bt.n_runs == 1 ? Range{bt.run_start[0], bt.run_end[0]} : Range{0, 0}; }
 
-template <int NR, int NF, int D, int KW, int W>
+template <int NR, int NF, int D, int KW, int WR, int W>
 hipError_t gate_up(const W4Args &a, const BranchTable &bt)
 {
     int groups = 0;                          // an upper bound: a group shared by two branches counts for both
@@ -325,35 +340,37 @@ hipError_t gate_up(const W4Args &a, const BranchTable &bt)
     for (int b = 0; b < bt.B; ++b)
         if (((bt.active >> b) & 1) && bt.off[b + 1] > bt.off[b]) groups += ceil_div(bt.off[b + 1], 16) - bt.off[b] / 16;
     if (one) groups = ceil_div(run.end, 16) - run.beg / 16;
-    const int row_tiles = ceil_div(groups, kWaves * NR), token_tiles = ceil_div(a.T, 16 * NF);
-    const size_t lds = KW * core_lds(2 * NR, NF, D);
-    const hipError_t e = one ? allow_lds<w4_tile_gate_up<NR, NF, D, KW, W, true>>((int)lds, "w4_tile_gate_up attribute")
-                             : allow_lds<w4_tile_gate_up<NR, NF, D, KW, W, false>>((int)lds, "w4_tile_gate_up attribute");
+    const int row_tiles = ceil_div(groups, WR * NR), token_tiles = ceil_div(a.T, 16 * NF);
+    const size_t lds = core_lds(2 * NR, NF, D, KW, WR);
+    const hipError_t e = one ? allow_lds<w4_tile_gate_up<NR, NF, D, KW, WR, W, true>>((int)lds, "w4_tile_gate_up attribute")
+                             : allow_lds<w4_tile_gate_up<NR, NF, D, KW, WR, W, false>>((int)lds, "w4_tile_gate_up attribute");
     if (e != hipSuccess) return e;
     ProfileScope ps(MLPMOE_KERNEL_W4_GATE_UP, a.stream);
-    (one ? w4_tile_gate_up<NR, NF, D, KW, W, true> : w4_tile_gate_up<NR, NF, D, KW, W, false>)
-        <<<ceil_div(row_tiles, 8) * 8 * token_tiles, KW * kWaves * 64, lds, a.stream>>>(
+    (one ? w4_tile_gate_up<NR, NF, D, KW, WR, W, true> : w4_tile_gate_up<NR, NF, D, KW, WR, W, false>)
+        <<<dim3(8, token_tiles, ceil_div(row_tiles, 8)), KW * WR * 64, lds, a.stream>>>(
             static_cast<const uint16_t *>(a.x), a.T, a.d_model, a.d_inter, a.gc, a.gs, a.uc, a.us, static_cast<uint16_t *>(a.H), a.ldh, a.route,
-            row_tiles, token_tiles, run, bt);
+            row_tiles, run, bt);
     return launch_status("w4_tile_gate_up launch");
 }
 
-template <int NA, int NF, int D, int KW, int W>
+template <int NA, int NF, int D, int KW, int WR, int W>
 hipError_t down(const W4Args &a, const BranchTable &bt, int splits)
 {
-    const int row_tiles = ceil_div(a.d_model, 16 * kWaves * NA), token_tiles = ceil_div(a.T, 16 * NF);
+    int log_splits = 0;
+    while (1 << log_splits < splits) ++log_splits;
+    const int row_tiles = ceil_div(a.d_model, 16 * WR * NA), token_tiles = ceil_div(a.T, 16 * NF);
     const Range run = run_of(a, bt);
     const bool one = run.end > 0;
-    const size_t lds = KW * core_lds(NA, NF, D) + (one ? 0 : (size_t)ceil_div(a.d_inter / 32, 32) * 4);
-    hipError_t e = one ? allow_lds<w4_tile_down<NA, NF, D, KW, W, true>>((int)lds, "w4_tile_down attribute")
-                       : allow_lds<w4_tile_down<NA, NF, D, KW, W, false>>((int)lds, "w4_tile_down attribute");
+    const size_t lds = core_lds(NA, NF, D, KW, WR) + (one ? 0 : (size_t)ceil_div(a.d_inter / 32, 32) * 4 + (size_t)ceil_div(a.d_inter, kStepK) * 2);
+    hipError_t e = one ? allow_lds<w4_tile_down<NA, NF, D, KW, WR, W, true>>((int)lds, "w4_tile_down attribute")
+                       : allow_lds<w4_tile_down<NA, NF, D, KW, WR, W, false>>((int)lds, "w4_tile_down attribute");
     if (e != hipSuccess) return e;
     {
         ProfileScope ps(MLPMOE_KERNEL_W4_DOWN, a.stream);
-        (one ? w4_tile_down<NA, NF, D, KW, W, true> : w4_tile_down<NA, NF, D, KW, W, false>)
-            <<<ceil_div(row_tiles * splits, 8) * 8 * token_tiles, KW * kWaves * 64, lds, a.stream>>>(
-                static_cast<const uint16_t *>(a.H), a.ldh, a.T, a.d_inter, a.dc, a.ds, a.d_model, a.out, a.out_bf16, a.partial, splits,
-                a.route, row_tiles, token_tiles, run, bt);
+        (one ? w4_tile_down<NA, NF, D, KW, WR, W, true> : w4_tile_down<NA, NF, D, KW, WR, W, false>)
+            <<<dim3(8, token_tiles << log_splits, ceil_div(row_tiles, 8)), KW * WR * 64, lds, a.stream>>>(
+                static_cast<const uint16_t *>(a.H), a.ldh, a.T, a.d_inter, a.dc, a.ds, a.d_model, a.out, a.out_bf16, a.partial, log_splits,
+                a.route, row_tiles, run, bt);
         e = launch_status("w4_tile_down launch");
         if (e != hipSuccess || splits == 1) return e;
     }
@@ -366,29 +383,54 @@ hipError_t down(const W4Args &a, const BranchTable &bt, int splits)
 
 }  // namespace
 
-// K ranges of the down projection: enough workgroups to fill the chip twice.
-int w4_splits(int T, int d_model, int d_inter)
+// Tiles of the down projection: 128 features x 32, 48 or 64 tokens while there are few, 256 x 64 where that gives 64 tiles; and K
+// cut until there are two workgroups a CU.  us, down projection and the sum of its ranges:
+//   4096 x 14336: T = 24 128 x 32 20.8, 128 x 64 23.7; T = 45 128 x 48 24.2, 128 x 64 24.7; T = 128 128 x 64 32.8, 256 x 64 36.6; T = 200 256 x 64 47.2,
+//   128 x 64 48.6; T = 500 75.2 and 82.3; T = 1000 127 and 145
+//   896 x 4864: T = 500 128 x 64 22.9, 256 x 64 more than 26; T = 2000 41 and more than 49
+struct DownTile {
+    int kind, rows, tokens, splits;
+};
+DownTile down_tile(int T, int d_model, int d_inter)
 {
-    const int tiles = ceil_div(d_model, 256) * ceil_div(T, 64);
-    int s = 1;
-    while (s < 8 && tiles * s * 2 <= 512) s *= 2;
-    return s;
+    DownTile t = T <= 32 ? DownTile{0, 128, 32, 1} : T <= 48 ? DownTile{1, 128, 48, 1} : T <= 64 ? DownTile{2, 128, 64, 1} : DownTile{3, 128, 64, 1};
+    if (T > 64 && d_model >= 1024 && (long long)ceil_div(d_model, 256) * ceil_div(T, 64) >= 64) t = DownTile{4, 256, 64, 1};
+    const long long tiles = (long long)ceil_div(d_model, t.rows) * ceil_div(T, t.tokens);
+    while (t.splits < 8 && tiles * t.splits * 2 <= 512 && d_inter >= kStepK * 8 * t.splits) t.splits *= 2;
+    return t;
 }
 
+int w4_splits(int T, int d_model, int d_inter) { return down_tile(T, d_model, d_inter).splits; }
+
+// Tiles of gate+up: 64 neurons x 32 or 48 tokens while there are few, then by what still fills the chip: 256 x 128 (8 waves, for
+// a K worth its start), 128 x 64 or 64 x 64.  us:
+//   4096 x 14336: T = 45 64 x 48 25.6, 64 x 32 38.4; T = 64 64 x 32 37.0, 64 x 64 38.4; T = 128 64 x 64 44.9, 128 x 64 51.7; T = 200 128 x 64
+//   69.7, 64 x 64 82.4; T = 300 102.9, 256 x 128 104.9; T = 500 256 x 128 103.5 .. 112, 128 x 64 124; T = 2000 431 and 476
+//   2048 x 7168: T = 200 64 x 64 26.7, 128 x 64 30.3; T = 300 41.2 and 35.5; T = 1000 256 x 128 65.0, 128 x 64 70.2
+//   896 x 4864: T = 500 128 x 64 24.0, 64 x 64 25.0, 256 x 128 33.7; T = 2000 51.8, 61.9, 65.9
 hipError_t launch_w4_tiles(const W4Args &a, const BranchTable &bt)
 {
-    const int s = w4_splits(a.T, a.d_model, a.d_inter);
+    const int n = bt.d_eff;
     hipError_t e;
-    if (a.T <= 48) {
-        e = gate_up<1, 3, 3, 2, 2>(a, bt);
-        return e == hipSuccess ? down<2, 3, 3, 2, 2>(a, bt, s) : e;
+    if (a.T <= 32 || (a.T > 48 && a.T <= 64))
+        e = gate_up<1, 2, 2, 2, 4, 2>(a, bt);
+    else if (a.T <= 48)
+        e = gate_up<1, 3, 2, 2, 4, 2>(a, bt);
+    else if (a.d_model >= 2048 && (long long)ceil_div(n, 256) * ceil_div(a.T, 128) >= 200)
+        e = gate_up<2, 8, 1, 1, 8, 2>(a, bt);
+    else if ((long long)ceil_div(n, 128) * ceil_div(a.T, 64) >= 256)
+        e = gate_up<2, 4, 1, 1, 4, 2>(a, bt);
+    else
+        e = gate_up<1, 4, 1, 1, 4, 3>(a, bt);
+    if (e != hipSuccess) return e;
+    const DownTile t = down_tile(a.T, a.d_model, a.d_inter);
+    switch (t.kind) {
+    case 0: return down<2, 2, 2, 2, 4, 2>(a, bt, t.splits);
+    case 1: return down<2, 3, 2, 2, 4, 2>(a, bt, t.splits);
+    case 2: return down<2, 4, 2, 1, 4, 2>(a, bt, t.splits);
+    case 3: return down<2, 4, 1, 1, 4, 3>(a, bt, t.splits);
+    default: return down<4, 4, 1, 1, 4, 2>(a, bt, t.splits);
     }
-    if (a.T <= 192) {
-        e = gate_up<1, 4, 3, 1, 2>(a, bt);
-        return e == hipSuccess ? down<2, 4, 3, 1, 2>(a, bt, s) : e;
-    }
-    e = gate_up<2, 4, 1, 1, 2>(a, bt);
-    return e == hipSuccess ? down<4, 4, 1, 1, 2>(a, bt, s) : e;
 }
 
 }  // namespace mlpmoe

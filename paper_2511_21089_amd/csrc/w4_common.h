@@ -208,38 +208,22 @@ struct Groups {
     }
 };
 
-// h of 4 neurons n .. n + 3 (this lane's) of a group n0 .. n0 + G - 1 (uniform) for F tokens, as bf16: alpha SiLU(g) u, or 0 where the
-// neuron's branch is off or the token does not take it.  store(token, 8 bytes).  All lanes of the wave call it.
-template <int G, int F, typename Value, typename Takes, typename Store>
-__device__ __forceinline__ void gated(const BranchLanes &br, const BranchTable &bt, int n0, int n, Value value, Takes takes, Store store)
+// h of 4 neurons n .. n + 3 (this lane's) of a group n0 .. n0 + G - 1 (uniform) from gate and up sums, as bf16: alpha SiLU(g) u, or 0 where
+// the neuron's branch is off or the token does not take it.  store(8 bytes).  All lanes of the wave call it.
+template <int G, typename Takes, typename Store>
+__device__ __forceinline__ void gated(const BranchLanes &br, const BranchTable &bt, int n0, int n, f32x4 g, f32x4 u, Takes takes, Store store)
 {
-    const int b0 = br.branch(n0);
-    const bool one = br.next(b0) >= n0 + G;             // the whole group is in one branch
-    const float alpha0 = br.alpha(b0);
-    const bool on0 = (bt.active >> b0) & 1;
-    float alpha[4];
-    int branch[4];
+    int b = br.branch(n0), end = br.next(b);
+    f32x4 h = {0, 0, 0, 0};
+#pragma unroll 1
+    for (int beg = n0; beg < n0 + G; beg = end, ++b, end = br.next(b)) {         // mostly once: the group lies in one branch
+        if (!((bt.active >> b) & 1) || !takes(b)) continue;
+        const float alpha = br.alpha(b);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) alpha[e] = alpha0, branch[e] = on0 ? b0 : -1;
-    if (!one)
-        for (int b = b0 + 1, beg = br.next(b0); beg < n0 + G; beg = br.next(b), ++b) {
-            const float a = br.alpha(b);
-            const bool on = (bt.active >> b) & 1;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (n + e >= beg) alpha[e] = a, branch[e] = on ? b : -1;
-        }
-#pragma unroll
-    for (int f = 0; f < F; ++f) {
-        uint16_t h[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float g, u;
-            value(f, e, g, u);
-            h[e] = branch[e] >= 0 && takes(f, branch[e]) ? to_bf16(alpha[e] * silu_mul(g, u)) : (uint16_t)0;
-        }
-        store(f, uint2{(uint32_t)h[0] | (uint32_t)h[1] << 16, (uint32_t)h[2] | (uint32_t)h[3] << 16});
+        for (int e = 0; e < 4; ++e)
+            if (n + e >= beg && n + e < end) h[e] = alpha * silu_mul(g[e], u[e]);
     }
+    store(uint2{(uint32_t)to_bf16(h[0]) | (uint32_t)to_bf16(h[1]) << 16, (uint32_t)to_bf16(h[2]) | (uint32_t)to_bf16(h[3]) << 16});
 }
 
 // The down projection reads H by whole steps of 128 neurons.  Groups of G that a live branch reaches into are written whole;
@@ -284,6 +268,22 @@ __device__ __forceinline__ void mark_blocks(const OffsetLanes &off, unsigned lon
         bits[i] = w;
     }
     __syncthreads();
+}
+
+// The steps of K with a live block, in order: every wave counts them, all write the same list.  Ends with a barrier.
+__device__ __forceinline__ int list_steps(const uint32_t *bits, int all, uint16_t *list)
+{
+    int n = 0;
+#pragma unroll 1
+    for (int s = 0; s < all; s += 64) {
+        const int st = s + (threadIdx.x & 63);
+        const bool on = st < all && ((bits[st / 8] >> (st % 8 * 4)) & 15u) != 0;
+        const unsigned long long m = __ballot(on);
+        if (on) list[n + __popcll(m & ((1ULL << (threadIdx.x & 63)) - 1))] = (uint16_t)st;
+        n += __popcll(m);
+    }
+    __syncthreads();
+    return n;
 }
 
 // Lets a kernel have `bytes` of LDS on the current device: the runtime is asked when a call needs more than those before it
