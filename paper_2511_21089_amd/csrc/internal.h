@@ -138,6 +138,10 @@ int owned_workspace(size_t need, size_t least, hipStream_t stream, void **ptr, s
 
 // The router (kernels_route.hip).
 constexpr int kRouteMaxBlocks = 256;
+struct RoutePart {
+    float p;
+    int c;
+};
 struct RouteArgs {
     const void *logits;
     int ld, T, B, k, elem_bytes, n_active;
@@ -147,8 +151,8 @@ struct RouteArgs {
     float *probs;                     // or nullptr
     int32_t *counts;                  // [B + 1], or nullptr
     float *loss;                      // or nullptr
-    float *part_p;                    // partial sums of more than one block
-    int *part_c;
+    RoutePart *part;                  // partial sums of more than one block, [blocks][B], and their tokens, [blocks]
+    int *part_n;
     hipStream_t stream;
 };
 struct RouteBackArgs {

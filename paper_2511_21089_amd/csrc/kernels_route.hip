@@ -19,15 +19,14 @@ typedef __attribute__((ext_vector_type(4))) uint16_t u16x4;
 constexpr float kNegInf = -__builtin_inff();
 
 template <int kCtrl>
-__device__ __forceinline__ float dpp(float v)
-{
-    const int i = __builtin_bit_cast(int, v);
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, kCtrl, 0xf, 0xf, false));
-}
-template <int kCtrl>
 __device__ __forceinline__ int dpp(int v)
 {
-    return __builtin_amdgcn_update_dpp(v, v, kCtrl, 0xf, 0xf, false);
+    return __builtin_amdgcn_update_dpp(0, v, kCtrl, 0xf, 0xf, true);
+}
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float v)
+{
+    return __builtin_bit_cast(float, dpp<kCtrl>(__builtin_bit_cast(int, v)));
 }
 
 // Reduction over the L lanes of a token, the same value on each: neighbours, pairs, then the mirrored half and the mirrored
@@ -46,9 +45,28 @@ struct Add {
     __device__ __forceinline__ V operator()(V a, V b) const { return a + b; }
 };
 struct Max {
-    // a not-a-number loses against a number
-    __device__ __forceinline__ float operator()(float a, float b) const { return __builtin_fmaxf(a, b); }
+    __device__ __forceinline__ int operator()(int a, int b) const { return a > b ? a : b; }
 };
+
+// Logits as integers in the same order, both zeros alike and what is not a number as -inf: the largest of two is one
+// instruction that takes its operand across lanes, where a float's needs two more to be quiet about not-a-numbers.
+__device__ __forceinline__ int order(float x)
+{
+    const int i = __builtin_bit_cast(int, (x > kNegInf ? x : kNegInf) + 0.0f);
+    return i ^ ((i >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float value(int o) { return __builtin_bit_cast(float, o ^ ((o >> 31) & 0x7fffffff)); }
+
+// One lane out of each L: of the lanes that are set, the lowest of each L.  Every L has one set, or none and then no later one
+// either, so the carry of a sum stays where it began.
+template <int L>
+__device__ __forceinline__ bool lowest(bool set)
+{
+    if (L == 1) return set;
+    constexpr unsigned long long kOnes = ~0ULL / ((1ULL << L) - 1);
+    const unsigned long long m = __ballot(set);
+    return __builtin_amdgcn_inverse_ballot_w64(m & (~m + kOnes));
+}
 
 __device__ __forceinline__ float widen(uint16_t v) { return __builtin_bit_cast(float, (uint32_t)v << 16); }
 __device__ __forceinline__ float widen(float v) { return v; }
@@ -102,136 +120,133 @@ __device__ __forceinline__ void store4(uint16_t *row, int b0, int B, const float
     }
 }
 
-// Sums of a call with counts and loss from the blocks' partial sums, in the order of the blocks; the probabilities' in
-// double, since the number of tokens goes to 2^24.
-__device__ __forceinline__ void finish(const float *psum, const int *cnt, int blocks, int B, int n_active, int32_t *counts,
-                                       float *loss)
+template <typename V>
+__device__ __forceinline__ V over_wave(V v)
 {
-    // psum and cnt: [blocks][B + 1], the last entry of a row the block's counted tokens
-    __shared__ double s_p[1024];
-    __shared__ int s_c[1024];
-    __shared__ double s_prod[64];
-    __shared__ int s_cnt[65];
-    const int cols = B + 1;
-    const int parts = (int)blockDim.x / cols;            // threads that share a column
-    const int col = threadIdx.x % cols, part = threadIdx.x / cols;
-    double p = 0;
-    int c = 0;
-    if (part < parts)
-        for (int i = part; i < blocks; i += parts) {
-            p += (double)psum[(size_t)i * cols + col];
-            c += cnt[(size_t)i * cols + col];
-        }
-    s_p[threadIdx.x] = p;
-    s_c[threadIdx.x] = c;
-    __syncthreads();
-    if ((int)threadIdx.x < cols) {
-        p = 0, c = 0;
-        for (int i = 0; i < parts; ++i) {
-            p += s_p[i * cols + threadIdx.x];
-            c += s_c[i * cols + threadIdx.x];
-        }
-        s_cnt[threadIdx.x] = c;
-        if (counts) counts[threadIdx.x] = c;
-        if ((int)threadIdx.x < B) s_prod[threadIdx.x] = p * (double)c;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0 && loss) {
-        double sum = 0;
-        long long taken = 0;
-        for (int b = 0; b < B; ++b) {
-            sum += s_prod[b];
-            taken += s_cnt[b];
-        }
-        const double n = (double)s_cnt[B];
-        *loss = taken > 0 ? (float)((double)n_active * sum / ((double)taken * n)) : 0.0f;
-    }
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
+    return v;
 }
 
-constexpr int kRouteThreads = 512;
+// Counts and loss from the sums over all tokens: lane b of the first wave has branch b's probabilities and count (zeros past B),
+// every lane the number of tokens.
+__device__ __forceinline__ void finish(double p, int c, int tokens, int B, int n_active, int32_t *counts, float *loss)
+{
+    const int lane = threadIdx.x;
+    if (counts && lane < B) counts[lane] = c;
+    if (counts && lane == 0) counts[B] = tokens;
+    const double sum = over_wave(p * (double)c), taken = over_wave((double)c);
+    if (loss && lane == 0) *loss = taken > 0 ? (float)((double)n_active * sum / (taken * (double)tokens)) : 0.0f;
+}
 
-// A token on L lanes, four branches a lane.  kStats: also what the counts and the loss need: with one block the result, else
-// the block's partial sums.
+constexpr int kRouteThreads = 1024;
+
+// A token on L lanes, four branches a lane; a wave's next tokens are asked for before these are worked on.  Bound by the
+// vector instructions of the k rounds, TODO.  kStats: also what the
+// counts and the loss need: with one block the result, else the block's partial sums, rows of B and the number of tokens.
 template <int L, typename E, bool kVec, bool kStats>
 __global__ void __launch_bounds__(kRouteThreads)
 route_topk_kernel(const E *__restrict__ logits, int ld, unsigned long long active, const uint8_t *__restrict__ token_mask,
-                  int T, int B, int k, uint8_t *__restrict__ route, float *__restrict__ probs, float *__restrict__ part_p,
-                  int *__restrict__ part_c, int32_t *__restrict__ counts, float *__restrict__ loss, int n_active)
+                  int T, int B, int k, uint8_t *__restrict__ route, float *__restrict__ probs, RoutePart *__restrict__ part,
+                  int *__restrict__ part_n, int32_t *__restrict__ counts, float *__restrict__ loss, int n_active)
 {
     const int l = threadIdx.x % L, b0 = 4 * l;
     const int per_block = blockDim.x / L;
+    const long long stride = (long long)gridDim.x * per_block;
     float sum_p[4] = {0, 0, 0, 0};
     int sum_c[4] = {0, 0, 0, 0}, sum_n = 0;
     const unsigned on = (unsigned)(active >> b0) & 15u;
-    // lanes of this token that come before this one
-    const unsigned long long lower = ((1ULL << l) - 1) << ((threadIdx.x & 63) - l);
 
-    for (long long t = (long long)blockIdx.x * per_block + threadIdx.x / L; t < T; t += (long long)gridDim.x * per_block) {
+    float ahead[4];
+    int real = 1;
+    long long t = (long long)blockIdx.x * per_block + threadIdx.x / L;
+    const E *row = logits + t * ld;
+    const long long row_step = stride * ld, out_step = stride * B;
+    const uint8_t *mask = token_mask + (token_mask ? t : 0);
+    float *to_probs = probs + (probs ? t * B : 0);
+    uint8_t *to_route = route + t * B;
+    if (t < T) {
+        load4<kVec>(row, b0, B, kNegInf, ahead);
+        if (token_mask) real = *mask;
+    }
+#pragma unroll 1
+    for (; t < T; t += stride) {
         float x[4];
-        load4<kVec>(logits + t * ld, b0, B, kNegInf, x);
-        const bool real = !token_mask || token_mask[t] != 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = ((on >> e) & 1u) && real ? x[e] : kNegInf;
-        const float m = over_token<L>(__builtin_fmaxf(__builtin_fmaxf(x[0], x[1]), __builtin_fmaxf(x[2], x[3])), Max());
-        const bool used = m > kNegInf;
+        for (int e = 0; e < 4; ++e) x[e] = ((on >> e) & 1u) && real != 0 ? ahead[e] : kNegInf;
+        if (t + stride < T) {
+            row += row_step;
+            load4<kVec>(row, b0, B, kNegInf, ahead);
+            if (token_mask) real = *(mask += stride);
+        }
+        int o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = order(x[e]);
+        // sorted, s[0] the largest
+        const Max more;
+        auto less = [](int a, int b) { return a < b ? a : b; };
+        int s[4];
+        {
+            const int a = more(o[0], o[1]), b = less(o[0], o[1]), c = more(o[2], o[3]), d = less(o[2], o[3]);
+            const int e = less(a, c), f = more(b, d);
+            s[0] = more(a, c);
+            s[1] = more(e, f);
+            s[2] = less(e, f);
+            s[3] = less(b, d);
+        }
+        const int none = order(kNegInf);
+        const int most = over_token<L>(s[0], more);
+        const bool used = most > none;
 
         float p[4] = {0, 0, 0, 0};
         if (probs || kStats) {
-            float s = 0;
+            const float m = value(most);
+            float sum = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 p[e] = __expf(x[e] - m);
-                s += p[e];
+                sum += p[e];
             }
-            s = over_token<L>(s, Add());
-            const float inv = 1.0f / s;
+            sum = over_token<L>(sum, Add());
+            // a reciprocal good to one unit in the last place, then one step of Newton's method
+            float inv = __builtin_amdgcn_rcpf(sum);
+            inv = inv * (2.0f - sum * inv);
 #pragma unroll
             for (int e = 0; e < 4; ++e) p[e] = used && x[e] != kNegInf ? p[e] * inv : 0.0f;
-            if (probs) store4<kVec>(probs + t * B, b0, B, p);
+            if (probs) store4<kVec>(to_probs, b0, B, p);
         }
 
-        // The k first in the order (larger logit, then lower index).  A lane sorts its four; every round takes the largest head
-        // of the token's lanes, of the lowest lane that has it.  What is not a number is never taken.
-        float y[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = x[e] > kNegInf ? x[e] : kNegInf;
+        // The k first in the order (larger logit, then lower index).  Every round takes the largest head of the token's lanes, of
+        // the lowest lane that has it; what is not there (-inf) comes last and is left out at the end.
         int rank[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int f = e + 1; f < 4; ++f) {
-                const int later = y[e] >= y[f];
+                const int later = o[e] >= o[f];
                 rank[f] += later;
                 rank[e] += 1 - later;
             }
-        float s0 = __builtin_fmaxf(y[0], y[1]), s1 = __builtin_fminf(y[0], y[1]);
-        float s2 = __builtin_fmaxf(y[2], y[3]), s3 = __builtin_fminf(y[2], y[3]);
-        float h = __builtin_fminf(s0, s2);
-        s0 = __builtin_fmaxf(s0, s2);
-        float lo = __builtin_fmaxf(s1, s3);
-        s3 = __builtin_fminf(s1, s3);
-        s1 = __builtin_fmaxf(h, lo);
-        s2 = __builtin_fminf(h, lo);
-        int taken = 0;
-        for (int i = 0; i < k; ++i) {
-            const float best = over_token<L>(s0, Max());
-            const bool mine = s0 == best && best > kNegInf;
-            const bool first = mine && (__ballot(mine) & lower) == 0;
+        int taken = 0, best = most;
+#pragma unroll 1
+        for (int i = k; i > 0; --i) {
+            const bool first = lowest<L>(s[0] == best);
             taken += first;
-            s0 = first ? s1 : s0;
-            s1 = first ? s2 : s1;
-            s2 = first ? s3 : s2;
-            s3 = first ? kNegInf : s3;
+            s[0] = first ? s[1] : s[0];
+            s[1] = first ? s[2] : s[1];
+            s[2] = first ? s[3] : s[2];
+            s[3] = first ? none : s[3];
+            best = over_token<L>(s[0], more);
         }
         uint32_t bytes = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) bytes |= (rank[e] < taken ? 1u : 0u) << (8 * e);
+        for (int e = 0; e < 4; ++e) bytes |= (rank[e] < taken && o[e] > none ? 1u : 0u) << (8 * e);
         if constexpr (kVec) {
-            if (b0 < B) *reinterpret_cast<uint32_t *>(route + t * B + b0) = bytes;
+            if (b0 < B) *reinterpret_cast<uint32_t *>(to_route + b0) = bytes;
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (b0 + e < B) route[t * B + b0 + e] = (uint8_t)(bytes >> (8 * e));
+                if (b0 + e < B) to_route[b0 + e] = (uint8_t)(bytes >> (8 * e));
         }
         if constexpr (kStats) {
 #pragma unroll
@@ -241,54 +256,85 @@ route_topk_kernel(const E *__restrict__ logits, int ld, unsigned long long activ
             }
             sum_n += used;
         }
+        to_probs += probs ? out_step : 0;
+        to_route += out_step;
     }
 
     if constexpr (kStats) {
-        // the block's sums, in the order of its tokens' lanes
-        __shared__ float s_p[kRouteThreads * 4];
-        __shared__ int s_c[kRouteThreads * 4];
-        __shared__ int s_n[kRouteThreads];
-        __shared__ float s_tp[65];
-        __shared__ int s_tc[65];
+        // over the tokens of a wave by lanes, then over the waves in their order
+        __shared__ float s_p[kRouteThreads / 64][64];
+        __shared__ int s_c[kRouteThreads / 64][64], s_n[kRouteThreads / 64];
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            s_p[threadIdx.x * 4 + e] = sum_p[e];
-            s_c[threadIdx.x * 4 + e] = sum_c[e];
+        for (int d = 32; d >= L; d /= 2) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sum_p[e] += __shfl_xor(sum_p[e], d);
+                sum_c[e] += __shfl_xor(sum_c[e], d);
+            }
+            sum_n += __shfl_xor(sum_n, d);
         }
-        s_n[threadIdx.x] = sum_n;
+        if (lane < L) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s_p[wave][b0 + e] = sum_p[e], s_c[wave][b0 + e] = sum_c[e];
+        }
+        if (lane == 0) s_n[wave] = sum_n;
         __syncthreads();
-        if ((int)threadIdx.x <= B) {
-            float p = 0;
-            int c = 0;
-            const int col = threadIdx.x;
-            for (int g = 0; g < per_block; ++g) {
-                if (col < B) {
-                    p += s_p[g * L * 4 + col];
-                    c += s_c[g * L * 4 + col];
-                } else {
-                    c += s_n[g * L];
-                }
-            }
-            if (gridDim.x == 1) {
-                s_tp[col] = p;
-                s_tc[col] = c;
-            } else {
-                part_p[(size_t)blockIdx.x * (B + 1) + col] = p;
-                part_c[(size_t)blockIdx.x * (B + 1) + col] = c;
-            }
+        if (wave > 0) return;
+        float p = 0;
+        int c = 0, n = 0;
+        for (int w = 0; w < waves; ++w) {
+            if (lane < 4 * L) p += s_p[w][lane], c += s_c[w][lane];
+            n += s_n[w];
         }
         if (gridDim.x == 1) {
-            __syncthreads();
-            finish(s_tp, s_tc, 1, B, n_active, counts, loss);
+            finish((double)p, c, n, B, n_active, counts, loss);
+        } else {
+            if (lane < B) part[(size_t)blockIdx.x * B + lane] = RoutePart{p, c};
+            if (lane == 0) part_n[blockIdx.x] = n;
         }
     }
 }
 
+// The blocks' partial sums, a lane a branch and a wave every 16th block, all asked for at once: the latency of one load and of the
+// instructions' first fetch.  Probabilities in double, since the number of tokens goes to 2^24.
 __global__ void __launch_bounds__(1024)
-route_finish_kernel(const float *__restrict__ part_p, const int *__restrict__ part_c, int blocks, int B, int n_active,
+route_finish_kernel(const RoutePart *__restrict__ part, const int *__restrict__ part_n, int blocks, int B, int n_active,
                     int32_t *__restrict__ counts, float *__restrict__ loss)
 {
-    finish(part_p, part_c, blocks, B, n_active, counts, loss);
+    __shared__ double s_p[16][64];
+    __shared__ int s_c[16][64], s_n[kRouteMaxBlocks / 64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    constexpr int EACH = kRouteMaxBlocks / 16;
+    const int at = threadIdx.x < (unsigned)blocks ? part_n[threadIdx.x] : 0;
+    RoutePart v[EACH];
+    const RoutePart *from = part + (lane < B ? lane : 0);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int block = wave + 16 * i;
+        v[i] = from[(block < blocks ? block : 0) * B];
+    }
+    double p = 0;
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const bool in = wave + 16 * i < blocks;
+        p += in ? (double)v[i].p : 0.0;
+        c += in ? v[i].c : 0;
+    }
+    s_p[wave][lane] = p;
+    s_c[wave][lane] = c;
+    if (wave < kRouteMaxBlocks / 64) {
+        const int n = over_wave(at);
+        if (lane == 0) s_n[wave] = n;
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    p = 0, c = 0;
+    int n = 0;
+    for (int w = 0; w < 16; ++w) p += s_p[w][lane], c += s_c[w][lane];
+    for (int w = 0; w < kRouteMaxBlocks / 64; ++w) n += s_n[w];
+    finish(lane < B ? p : 0.0, lane < B ? c : 0, n, B, n_active, counts, loss);
 }
 
 template <int L, typename E, bool kVec>
@@ -332,27 +378,40 @@ route_backward_kernel(const float *__restrict__ probs, const int32_t *__restrict
     }
 }
 
+int lanes(int B) { return B <= 4 ? 1 : B <= 8 ? 2 : B <= 16 ? 4 : B <= 32 ? 8 : 16; }
+
+// Threads and blocks of a call with counts or loss.  One block, which needs no second kernel, while a thread has at most two
+// tokens; then 256 threads while that gives at most kRouteMaxBlocks blocks; then 1024, which fill the chip with a block on every CU.
+int route_threads(int T, int B)
+{
+    const long long all = (long long)T * lanes(B);
+    return all > 2 * kRouteThreads && all <= 256LL * kRouteMaxBlocks ? 256 : kRouteThreads;
+}
+
 bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 template <int L, typename E, bool kVec>
-hipError_t launch_topk(const RouteArgs &a, int blocks)
+hipError_t launch_topk(const RouteArgs &a)
 {
+    const int blocks = route_blocks(a.T, a.B);
     const bool stats = a.counts || a.loss;
+    const long long want = ((long long)a.T * L + 255) / 256;
+    const int free_blocks = (int)(want < 2048 ? want : 2048);
     {
         ProfileScope ps(MLPMOE_KERNEL_ROUTE_TOPK, a.stream);
         if (stats)
-            route_topk_kernel<L, E, kVec, true><<<blocks, kRouteThreads, 0, a.stream>>>(
-                static_cast<const E *>(a.logits), a.ld, a.active, a.token_mask, a.T, a.B, a.k, a.route, a.probs, a.part_p,
-                a.part_c, a.counts, a.loss, a.n_active);
+            route_topk_kernel<L, E, kVec, true><<<blocks, route_threads(a.T, a.B), 0, a.stream>>>(
+                static_cast<const E *>(a.logits), a.ld, a.active, a.token_mask, a.T, a.B, a.k, a.route, a.probs, a.part,
+                a.part_n, a.counts, a.loss, a.n_active);
         else
-            route_topk_kernel<L, E, kVec, false><<<blocks, kRouteThreads, 0, a.stream>>>(
+            route_topk_kernel<L, E, kVec, false><<<free_blocks, 256, 0, a.stream>>>(
                 static_cast<const E *>(a.logits), a.ld, a.active, a.token_mask, a.T, a.B, a.k, a.route, a.probs, nullptr,
                 nullptr, nullptr, nullptr, a.n_active);
     }
     hipError_t e = launch_status("route_topk launch");
     if (e != hipSuccess || !stats || blocks == 1) return e;
     ProfileScope ps(MLPMOE_KERNEL_ROUTE_FINISH, a.stream);
-    route_finish_kernel<<<1, 1024, 0, a.stream>>>(a.part_p, a.part_c, blocks, a.B, a.n_active, a.counts, a.loss);
+    route_finish_kernel<<<1, 1024, 0, a.stream>>>(a.part, a.part_n, blocks, a.B, a.n_active, a.counts, a.loss);
     return launch_status("route_finish launch");
 }
 
@@ -368,17 +427,15 @@ hipError_t launch_back(const RouteBackArgs &a)
     return launch_status("route_backward launch");
 }
 
-int lanes(int B) { return B <= 4 ? 1 : B <= 8 ? 2 : B <= 16 ? 4 : B <= 32 ? 8 : 16; }
-
 template <typename E, bool kVec>
-hipError_t topk_lanes(const RouteArgs &a, int blocks)
+hipError_t topk_lanes(const RouteArgs &a)
 {
     switch (lanes(a.B)) {
-    case 1: return launch_topk<1, E, kVec>(a, blocks);
-    case 2: return launch_topk<2, E, kVec>(a, blocks);
-    case 4: return launch_topk<4, E, kVec>(a, blocks);
-    case 8: return launch_topk<8, E, kVec>(a, blocks);
-    default: return launch_topk<16, E, kVec>(a, blocks);
+    case 1: return launch_topk<1, E, kVec>(a);
+    case 2: return launch_topk<2, E, kVec>(a);
+    case 4: return launch_topk<4, E, kVec>(a);
+    case 8: return launch_topk<8, E, kVec>(a);
+    default: return launch_topk<16, E, kVec>(a);
     }
 }
 
@@ -398,19 +455,20 @@ hipError_t back_lanes(const RouteBackArgs &a)
 
 int route_blocks(int T, int B)
 {
-    const int per_block = kRouteThreads / lanes(B);
-    const long long want = ((long long)T + per_block - 1) / per_block;
-    return (int)(want < 1 ? 1 : want < kRouteMaxBlocks ? want : kRouteMaxBlocks);
+    const long long all = (long long)T * lanes(B);
+    if (all <= 2 * kRouteThreads) return 1;
+    const int threads = route_threads(T, B);
+    const long long want = (all + threads - 1) / threads;
+    return (int)(want < kRouteMaxBlocks ? want : kRouteMaxBlocks);
 }
 
 hipError_t launch_route_topk(const RouteArgs &a)
 {
-    const int blocks = route_blocks(a.T, a.B);
     const bool f32 = a.elem_bytes == 4;
     // rows of whole 4-branch pieces, each on its own alignment: one load and one store a lane
     const bool vec = a.B % 4 == 0 && a.ld % 4 == 0 && aligned(a.logits, f32 ? 16 : 8) && aligned(a.probs, 16) && aligned(a.route, 4);
-    if (f32) return vec ? topk_lanes<float, true>(a, blocks) : topk_lanes<float, false>(a, blocks);
-    return vec ? topk_lanes<uint16_t, true>(a, blocks) : topk_lanes<uint16_t, false>(a, blocks);
+    if (f32) return vec ? topk_lanes<float, true>(a) : topk_lanes<float, false>(a);
+    return vec ? topk_lanes<uint16_t, true>(a) : topk_lanes<uint16_t, false>(a);
 }
 
 hipError_t launch_route_backward(const RouteBackArgs &a)

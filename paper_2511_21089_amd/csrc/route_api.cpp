@@ -7,8 +7,8 @@ using namespace mlpmoe;
 
 namespace {
 
-// Partial sums of a call with counts or loss: [blocks][B + 1] floats, then as many ints.
-size_t part_bytes(int blocks, int B) { return align_up((size_t)blocks * (B + 1) * 4, 256); }
+// Partial sums of a call with counts or loss: [blocks][B] pairs, then [blocks] ints.
+size_t part_bytes(int blocks, int B) { return align_up((size_t)blocks * B * sizeof(RoutePart), 256); }
 
 bool aligned_to(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -60,8 +60,8 @@ int route_topk(const void *logits, int ld, const uint8_t *active_mask, const uin
     a.probs = probs;
     a.counts = counts;
     a.loss = loss;
-    a.part_p = nullptr;
-    a.part_c = nullptr;
+    a.part = nullptr;
+    a.part_n = nullptr;
     a.stream = static_cast<hipStream_t>(stream);
 
     const int blocks = route_blocks(T, B);
@@ -74,8 +74,8 @@ int route_topk(const void *logits, int ld, const uint8_t *active_mask, const uin
             if (rc != MLPMOE_OK) return rc;
         }
         if (!workspace || workspace_bytes < need || !aligned_to(workspace, 256)) return MLPMOE_ERR_WORKSPACE;
-        a.part_p = static_cast<float *>(workspace);
-        a.part_c = reinterpret_cast<int *>(static_cast<char *>(workspace) + part_bytes(blocks, B));
+        a.part = static_cast<RoutePart *>(workspace);
+        a.part_n = reinterpret_cast<int *>(static_cast<char *>(workspace) + part_bytes(blocks, B));
     }
     const hipError_t e = launch_route_topk(a);
     if (e != hipSuccess && g_err_detail[0] == 0) (void)note_hip_error("kernel launch", e);
@@ -89,7 +89,8 @@ extern "C" {
 size_t mlpmoe_route_workspace_bytes(int T, int B)
 {
     if (T < 0 || T > (1 << 24) || B < 1 || B > MLPMOE_MAX_BRANCHES) return 0;
-    return 2 * part_bytes(route_blocks(T, B), B);
+    const int blocks = route_blocks(T, B);
+    return part_bytes(blocks, B) + align_up((size_t)blocks * sizeof(int), 256);
 }
 
 int mlpmoe_route_topk(const void *logits, int ld, const uint8_t *active_mask, const uint8_t *token_mask, int T, int B, int k,
