@@ -14,6 +14,7 @@
 namespace mlpmoe {
 namespace {
 
+constexpr int kCus = 256;
 constexpr int kScaleBuf = 1280;          // scales of a wave's rows for 512 of K: 16 bytes a row, or 20 in five loads of a dword
 
 constexpr int stage_bytes(int NA, int NF, int KW, int WR) { return KW * NF * 4096 + KW * WR * NA * 1024; }
@@ -402,26 +403,33 @@ DownTile down_tile(int T, int d_model, int d_inter)
 
 int w4_splits(int T, int d_model, int d_inter) { return down_tile(T, d_model, d_inter).splits; }
 
-// Tiles of gate+up: 64 neurons x 32 or 48 tokens while there are few, then by what still fills the chip: 256 x 128 (8 waves, for
-// a K worth its start), 128 x 64 or 64 x 64.  us:
-//   4096 x 14336: T = 45 64 x 48 25.6, 64 x 32 38.4; T = 64 64 x 32 37.0, 64 x 64 38.4; T = 128 64 x 64 44.9, 128 x 64 51.7; T = 200 128 x 64
-//   69.7, 64 x 64 82.4; T = 300 102.9, 256 x 128 104.9; T = 500 256 x 128 103.5 .. 112, 128 x 64 124; T = 2000 431 and 476
-//   2048 x 7168: T = 200 64 x 64 26.7, 128 x 64 30.3; T = 300 41.2 and 35.5; T = 1000 256 x 128 65.0, 128 x 64 70.2
-//   896 x 4864: T = 500 128 x 64 24.0, 64 x 64 25.0, 256 x 128 33.7; T = 2000 51.8, 61.9, 65.9
+// Tiles of gate+up, neurons x tokens: the smallest of 64 x 32, 48 or 64 in two sets of waves with which a workgroup on every CU
+// does it in one go; past that 256 x 128 (8 waves, for a K worth its start) where its rounds over the chip are three quarters
+// full, 128 x 64 in 4 waves where there is more than one for every CU, else in 8.  us, - not measured:
+//   4096 x 14336: T = 45 64 x 48 22.9, 64 x 64 29.3; T = 64 64 x 64 30.4, 64 x 32 34.7; T = 128 128 x 64 (8) 41.0, 64 x 64 55.1; T = 200
+//   128 x 64 (4) 65, (8) 79; T = 300 99.7, 256 x 128 105; T = 500 256 x 128 103.5, 128 x 64 (4) 124; T = 2000 431 and 476
+//   4096 x 28672: T = 45 128 x 64 (8) 44.2, 64 x 48 47.6; T = 300 128 x 64 (4) 160, 256 x 128 in two rounds of 1.3 205
+//   8192 x 8192: T = 80 64 x 48 38.6, 64 x 64 50.8, 64 x 32 57.6; T = 200 128 x 64 (8) 74.0, (4) 85.9
+//   2048 x 7168: T = 45 64 x 32 13.2, 64 x 48 15.0; T = 96 64 x 48 16.1, 64 x 64 18.9; T = 300 128 x 64 (4) 35.1; T = 1000 256 x 128 65.0, 128 x 64 (4) 70.2
+//   896 x 4864: T = 96 64 x 32 11.1, 64 x 48 12.9; T = 300 128 x 64 (8) 16.5, (4) 17.2
 hipError_t launch_w4_tiles(const W4Args &a, const BranchTable &bt)
 {
     const int n = bt.d_eff;
+    auto tiles = [&](int rows, int tokens) { return (long long)ceil_div(n, rows) * ceil_div(a.T, tokens); };
+    const long long most = tiles(256, 128);
     hipError_t e;
-    if (a.T <= 32 || (a.T > 48 && a.T <= 64))
+    if (a.T <= 32 || tiles(64, 32) <= kCus)
         e = gate_up<1, 2, 2, 2, 4, 2>(a, bt);
-    else if (a.T <= 48)
+    else if (tiles(64, 48) <= kCus)
         e = gate_up<1, 3, 2, 2, 4, 2>(a, bt);
-    else if (a.d_model >= 2048 && (long long)ceil_div(n, 256) * ceil_div(a.T, 128) >= 200)
+    else if (tiles(64, 64) <= kCus)
+        e = gate_up<1, 4, 1, 2, 4, 2>(a, bt);
+    else if (a.d_model >= 2048 && most * 4 >= (most + kCus - 1) / kCus * kCus * 3)
         e = gate_up<2, 8, 1, 1, 8, 2>(a, bt);
-    else if ((long long)ceil_div(n, 128) * ceil_div(a.T, 64) >= 256)
+    else if (tiles(128, 64) > kCus)
         e = gate_up<2, 4, 1, 1, 4, 2>(a, bt);
     else
-        e = gate_up<1, 4, 1, 1, 4, 3>(a, bt);
+        e = gate_up<1, 4, 2, 1, 8, 2>(a, bt);
     if (e != hipSuccess) return e;
     const DownTile t = down_tile(a.T, a.d_model, a.d_inter);
     switch (t.kind) {
