@@ -169,33 +169,38 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
     pipeline_barrier<0>();                               // loads past the end are still on their way into LDS
 }
 
-// Bytes of LDS of w4_down: S stages of nt tokens' H and of codes, a kilobyte that loads without a token fill, the scales, and
-// for tables that are no single run a bit a block and the list of live steps.
-size_t down_lds(int W, int S, int nt, int K, bool one)
+// Bytes of LDS of w4_down: S stages of codes and of nt tokens' H, or H whole beside them, a kilobyte that loads without a token
+// fill, the scales, and for tables that are no single run a bit a block and the list of live steps.
+__host__ __device__ constexpr int whole_row(int K) { return (K + 4 * kStepK - 1) / (4 * kStepK) * 1024 + 16; }
+size_t down_lds(int W, int S, int nt, int K, bool one, bool whole)
 {
-    return (size_t)S * (nt * (W * 256 + 16) + W * 1024) + 1024 + scale_bytes(K) + (one ? 0 : (size_t)ceil_div(K / 32, 32) * 4 + ceil_div(K, kStepK) * 2);
+    return (size_t)S * (W * 1024 + (whole ? 0 : nt * (W * 256 + 16))) + (whole ? (size_t)nt * whole_row(K) : 0) + 1024 + scale_bytes(K) +
+           (one ? 0 : (size_t)ceil_div(K / 32, 32) * 4 + ceil_div(K, kStepK) * 2);
 }
 
-// Grid (tiles of 16 features, token tiles of up to 4 NL).  A workgroup of W waves owns 16 rows of W_down; in every chunk of W
-// steps of K each wave has one, so that together the waves read W * 64 bytes of a row.  Codes and H go through LDS, S - 1
-// chunks ahead.  A step is live if a live branch has a neuron in it; the others are left out.  The waves' sums are added in
+// Grid (tiles of 16 features, token tiles of up to 4 NL or 16).  A workgroup of W waves owns 16 rows of W_down; in every chunk of W
+// steps of K each wave has one, so that together the waves read W * 64 bytes of a row.  Codes (each wave its own) and H (for the
+// workgroup) go through LDS, S - 1 chunks ahead, and the waves meet for every chunk; NL = 0: H of up to 16 tokens lies in LDS whole, and
+// after one meeting every wave goes at its own pace.  A step is live if a live branch has a neuron in it; the others are left out.  The waves' sums are added in
 // their order.
 template <bool kOneRun, int W, int NL, int S>
 __global__ void __launch_bounds__(W * 64)
 w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__restrict__ dc, const uint8_t *__restrict__ ds,
         int d_model, void *__restrict__ out, int out_bf16, const uint8_t *__restrict__ route, Range run, BranchTable bt)
 {
+    constexpr bool kWhole = NL == 0;
     constexpr int PARTS = W / 4;                         // kilobytes of a token's chunk of H
     constexpr int PER = NL + 1, AHEAD = S - 1;
     static_assert((AHEAD - 1) * PER < 63, "loads in flight");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, r16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int t0 = 4 * NL * blockIdx.y, nt = T - t0 < 4 * NL ? T - t0 : 4 * NL;
+    constexpr int TOKENS = kWhole ? 16 : 4 * NL;
+    const int t0 = TOKENS * blockIdx.y, nt = T - t0 < TOKENS ? T - t0 : TOKENS;
     const int blocks = K / 32, all = (K + kStepK - 1) / kStepK, m0 = blockIdx.x * 16;
-    constexpr int HROW = W * 256 + 16;
-    const int stage = nt * HROW + W * 1024;
-    char *scrap = lds + S * stage, *scales = scrap + 1024;
+    const int h_row = kWhole ? whole_row(K) : W * 256 + 16, h_stage = kWhole ? 0 : nt * h_row;
+    const int stage = h_stage + W * 1024;
+    char *all_h = lds + S * stage, *scrap = all_h + (kWhole ? nt * h_row : 0), *scales = scrap + 1024;
     uint32_t *bits = reinterpret_cast<uint32_t *>(scales + scale_bytes(K));
     uint16_t *list = reinterpret_cast<uint16_t *>(bits + (blocks + 31) / 32);
     const int s_beg = kOneRun ? run.beg / kStepK : 0;
@@ -218,27 +223,42 @@ w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__
             const int s = step_of(c * W + part * 4 + q);
             const bool on = s >= 0 && t < nt;
             dma16(on ? hb + (size_t)t * ldh * 2 + s * 256 + h_lane : reinterpret_cast<const char *>(g_zero16),
-                  t < nt ? dst + t * HROW + part * 1024 : scrap);
+                  t < nt ? dst + t * h_row + part * 1024 : scrap);
         }
         const int s = step_of(c * W + wave);
         dma16(s >= 0 ? reinterpret_cast<const char *>(codes + s * 64 + (s == all - 1 ? q_last : q * 16)) : reinterpret_cast<const char *>(g_zero16),
-              dst + nt * HROW + wave * 1024);
+              dst + h_stage + wave * 1024);
     };
     const int chunks = (steps + W - 1) / W;
     keep_order();
 #pragma unroll 1
     for (int c = 0; c < AHEAD; ++c) {
         issue(c, lds + c * stage);
-        if (c == 0) stage_scales(ds + (size_t)m0 * blocks, scales, K / 2, true, wave, W);
+        if (c == 0) {
+            if (kWhole)
+#pragma unroll 1
+                for (int part = wave; part * 4 < steps; part += W) {
+                    const int s = step_of(part * 4 + q);
+#pragma unroll 1
+                    for (int t = 0; t < nt; ++t)
+                        dma16(s >= 0 ? hb + (size_t)t * ldh * 2 + s * 256 + h_lane : reinterpret_cast<const char *>(g_zero16),
+                              all_h + t * h_row + part * 1024);
+                }
+            stage_scales(ds + (size_t)m0 * blocks, scales, K / 2, true, wave, W);
+        }
         keep_order();
     }
     f32x4 acc = {0, 0, 0, 0};
     const char *mine = lds, *end = lds + S * stage;
     char *fill = lds + AHEAD * stage;
-    const int hr = (r16 < nt ? r16 : 0) * HROW + wave * 256 + q * 64, wr = nt * HROW + wave * 1024 + lane * 16;
+    const int hr = (r16 < nt ? r16 : 0) * h_row + wave * 256 + q * 64, wr = h_stage + wave * 1024 + lane * 16;
+    if (kWhole) pipeline_barrier<(AHEAD - 1) * PER>();
 #pragma unroll 1
     for (int c = 0; c < chunks; ++c) {
-        pipeline_barrier<(AHEAD - 1) * PER>();
+        if (kWhole)
+            wait_loads<(AHEAD - 1) * PER>();
+        else
+            pipeline_barrier<(AHEAD - 1) * PER>();
         issue(c + AHEAD, fill);
         const int s = step_of(c * W + wave);
         if (s >= 0) {
@@ -248,9 +268,10 @@ w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__
             const bool on = b < blocks && (kOneRun ? b >= run.beg / 32 && b * 32 < run.end : (bits[b / 32] >> (b & 31) & 1) != 0);
             const float scale = scale_of(on ? byte : 127u);
             const u32x4 w = *reinterpret_cast<const u32x4 *>(mine + wr);
+            const char *mh = kWhole ? all_h + c * W * 256 : mine;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[j], scale), *reinterpret_cast<const bf16x8 *>(mine + hr + j * 16),
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[j], scale), *reinterpret_cast<const bf16x8 *>(mh + hr + j * 16),
                                                               acc, 0, 0, 0);
         }
         mine = mine + stage == end ? lds : mine + stage;
@@ -348,12 +369,12 @@ unsigned convert_blocks(size_t pieces)
 template <bool kOneRun, int W, int NL, int S>
 hipError_t launch_down(const W4Args &a, const BranchTable &bt, const Range &run)
 {
-    const int nt = a.T < 4 * NL ? a.T : 4 * NL;
-    const size_t lds = down_lds(W, S, nt, a.d_inter, kOneRun);
+    constexpr int TOKENS = NL == 0 ? 16 : 4 * NL;
+    const size_t lds = down_lds(W, S, a.T < TOKENS ? a.T : TOKENS, a.d_inter, kOneRun, NL == 0);
     const hipError_t e = allow_lds<w4_down<kOneRun, W, NL, S>>((int)lds, "w4_down attribute");
     if (e != hipSuccess) return e;
     ProfileScope ps(MLPMOE_KERNEL_W4_DOWN, a.stream);
-    w4_down<kOneRun, W, NL, S><<<dim3(a.d_model / 16, ceil_div(a.T, 4 * NL)), W * 64, lds, a.stream>>>(
+    w4_down<kOneRun, W, NL, S><<<dim3(a.d_model / 16, ceil_div(a.T, TOKENS)), W * 64, lds, a.stream>>>(
         static_cast<const uint16_t *>(a.H), a.ldh, a.T, a.d_inter, a.dc, a.ds, a.d_model, a.out, a.out_bf16, a.route, run, bt);
     return launch_status("w4_down launch");
 }
@@ -396,12 +417,15 @@ hipError_t gate_up(const W4Args &a, const BranchTable &bt, const Range &run, int
     return launch_gate_up<kOneRun, 4, 2>(a, bt, run, groups, 1, 4);      // scales of a very long K: one wave, four tokens at a time
 }
 
-// 16 waves while three stages of their chunks fit, else 8, whose chunks are half as long.
+// 16 waves while three stages of their chunks fit, else 8, whose chunks are half as long.  H whole if it fits for up to 8 tokens, us
+// against H by chunks: 4096 x 14336, T = 1 7.9, 8.7; 8192 x 8192, T = 1 12.2 and 13.5, T = 4 13.5 and 14.0; 2048 x 7168, T = 1 4.7 and 5.4,
+// T = 8 6.0 and 6.2, T = 12 7.0 and 6.4; 896 x 4864, T = 1 3.8 and 4.4.
 template <bool kOneRun>
 hipError_t down(const W4Args &a, const BranchTable &bt, const Range &run)
 {
     const int nt = a.T < 16 ? a.T : 16, K = a.d_inter;
-    auto fits = [&](int W, int S) { return down_lds(W, S, nt, K, kOneRun) <= (size_t)kLdsBytes; };
+    auto fits = [&](int W, int S, bool whole = false) { return down_lds(W, S, nt, K, kOneRun, whole) <= (size_t)kLdsBytes; };
+    if (nt <= 8 && fits(16, 4, true)) return launch_down<kOneRun, 16, 0, 4>(a, bt, run);
     if (nt <= 4 && fits(16, 4)) return launch_down<kOneRun, 16, 1, 4>(a, bt, run);
     if (nt <= 8 && fits(16, 3)) return launch_down<kOneRun, 16, 2, 3>(a, bt, run);
     if (fits(8, 3)) return launch_down<kOneRun, 8, 4, 3>(a, bt, run);
