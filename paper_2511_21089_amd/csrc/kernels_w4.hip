@@ -79,9 +79,9 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
         if (blockIdx.x == 0) clear_edges(run, H + (size_t)t0 * ldh, ldh, nt, wave, nw);
     } else {
         const OffsetLanes off(bt);
-        const unsigned long long live = live_of_16(bt, route, t0, nt);
+        const unsigned long long live = live_of_16(bt, route, 0, T);    // of all tokens: the down projection's tiles may be larger
         groups = Groups<8, kOneRun>(off, live);
-        if (blockIdx.x == 0) clear_edges(off, bt.B, live, H + (size_t)t0 * ldh, ldh, nt, wave, nw);
+        if (blockIdx.x == 0) clear_edges(off, bt.B, live, live, H + (size_t)t0 * ldh, ldh, nt, wave, nw);
     }
 
     // lane of a load of x: place 16 s + 4 q + j of the 64 is piece 16 q + 4 s + j

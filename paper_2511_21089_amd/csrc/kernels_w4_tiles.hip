@@ -180,11 +180,13 @@ __device__ __forceinline__ void each_sum(const f32x4 (&acc)[NA][NF], char *lds, 
 // weights, are on one XCD, one after the other.
 
 // A row wave takes NR groups of 16 neurons that a live branch reaches into, at multiples of 16: rows of W_gate, then of W_up.
+// reach: tokens of a workgroup of the down projection, which reads what any of them has live, so that a tile's tokens need zeros
+// there.
 template <int NR, int NF, int AHEAD, int KW, int WR, int W, bool kOneRun>
 __global__ void __launch_bounds__(KW * WR * 64, W)
 w4_tile_gate_up(const uint16_t *__restrict__ x, int T, int K, int d_inter, const uint8_t *__restrict__ gc, const uint8_t *__restrict__ gs,
                 const uint8_t *__restrict__ uc, const uint8_t *__restrict__ us, uint16_t *__restrict__ H, int ldh,
-                const uint8_t *__restrict__ route, int row_tiles, Range run, BranchTable bt)
+                const uint8_t *__restrict__ route, int reach, int row_tiles, Range run, BranchTable bt)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int row = blockIdx.z * 8 + blockIdx.x;
@@ -196,11 +198,13 @@ w4_tile_gate_up(const uint16_t *__restrict__ x, int T, int K, int d_inter, const
     if constexpr (kOneRun) {
         if (row == 0) clear_edges(run, H + (size_t)t0 * ldh, ldh, nt, wave, WR);
     } else {
-        __shared__ unsigned any[2];
+        __shared__ unsigned any[4];
         const OffsetLanes off(bt);
         const unsigned long long live = live_of(bt, route, t0, nt, any);
+        const int r0 = t0 / reach * reach, upto = (t0 + nt + reach - 1) / reach * reach, r1 = upto < T ? upto : T;
+        const unsigned long long wide = route && (r0 < t0 || r1 > t0 + nt) ? live_of(bt, route, r0, r1 - r0, any + 2) : live;
         groups = Groups<16, kOneRun>(off, live);
-        if (row == 0) clear_edges(off, bt.B, live, H + (size_t)t0 * ldh, ldh, nt, wave, WR);
+        clear_edges(off, bt.B, live, wide, H + (size_t)t0 * ldh, ldh, nt, row * WR + wave, row_tiles * WR);
         if (row * WR * NR >= groups.total) return;
     }
 
@@ -333,7 +337,7 @@ w4_reduce(const float *__restrict__ partial, size_t n4, int splits, void *__rest
 Range run_of(const W4Args &a, const BranchTable &bt) { return !a.route && bt.n_runs == 1 ? Range{bt.run_start[0], bt.run_end[0]} : Range{0, 0}; }
 
 template <int NR, int NF, int D, int KW, int WR, int W>
-hipError_t gate_up(const W4Args &a, const BranchTable &bt)
+hipError_t gate_up(const W4Args &a, const BranchTable &bt, int reach)
 {
     int groups = 0;                          // an upper bound: a group shared by two branches counts for both
     const Range run = run_of(a, bt);
@@ -350,7 +354,7 @@ hipError_t gate_up(const W4Args &a, const BranchTable &bt)
     (one ? w4_tile_gate_up<NR, NF, D, KW, WR, W, true> : w4_tile_gate_up<NR, NF, D, KW, WR, W, false>)
         <<<dim3(8, token_tiles, ceil_div(row_tiles, 8)), KW * WR * 64, lds, a.stream>>>(
             static_cast<const uint16_t *>(a.x), a.T, a.d_model, a.d_inter, a.gc, a.gs, a.uc, a.us, static_cast<uint16_t *>(a.H), a.ldh, a.route,
-            row_tiles, run, bt);
+            reach, row_tiles, run, bt);
     return launch_status("w4_tile_gate_up launch");
 }
 
@@ -415,23 +419,23 @@ int w4_splits(int T, int d_model, int d_inter) { return down_tile(T, d_model, d_
 hipError_t launch_w4_tiles(const W4Args &a, const BranchTable &bt)
 {
     const int n = bt.d_eff;
+    const DownTile t = down_tile(a.T, a.d_model, a.d_inter);
     auto tiles = [&](int rows, int tokens) { return (long long)ceil_div(n, rows) * ceil_div(a.T, tokens); };
     const long long most = tiles(256, 128);
     hipError_t e;
     if (a.T <= 32 || tiles(64, 32) <= kCus)
-        e = gate_up<1, 2, 2, 2, 4, 2>(a, bt);
+        e = gate_up<1, 2, 2, 2, 4, 2>(a, bt, t.tokens);
     else if (tiles(64, 48) <= kCus)
-        e = gate_up<1, 3, 2, 2, 4, 2>(a, bt);
+        e = gate_up<1, 3, 2, 2, 4, 2>(a, bt, t.tokens);
     else if (tiles(64, 64) <= kCus)
-        e = gate_up<1, 4, 1, 2, 4, 2>(a, bt);
+        e = gate_up<1, 4, 1, 2, 4, 2>(a, bt, t.tokens);
     else if (a.d_model >= 2048 && most * 4 >= (most + kCus - 1) / kCus * kCus * 3)
-        e = gate_up<2, 8, 1, 1, 8, 2>(a, bt);
+        e = gate_up<2, 8, 1, 1, 8, 2>(a, bt, t.tokens);
     else if (tiles(128, 64) > kCus)
-        e = gate_up<2, 4, 1, 1, 4, 2>(a, bt);
+        e = gate_up<2, 4, 1, 1, 4, 2>(a, bt, t.tokens);
     else
-        e = gate_up<1, 4, 2, 1, 8, 2>(a, bt);
+        e = gate_up<1, 4, 2, 1, 8, 2>(a, bt, t.tokens);
     if (e != hipSuccess) return e;
-    const DownTile t = down_tile(a.T, a.d_model, a.d_inter);
     switch (t.kind) {
     case 0: return down<2, 2, 2, 2, 4, 2>(a, bt, t.splits);
     case 1: return down<2, 3, 2, 2, 4, 2>(a, bt, t.splits);

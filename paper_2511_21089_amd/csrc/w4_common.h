@@ -12,7 +12,6 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-typedef __attribute__((ext_vector_type(4), aligned(1))) uint32_t u32x4_any;      // at any address
 
 typedef const __attribute__((address_space(1))) void *gptr_t;
 typedef __attribute__((address_space(3))) void *lptr_t;
@@ -89,34 +88,6 @@ constexpr int kStepK = 128;
 
 // Place of neuron n in a row of H.
 __device__ __forceinline__ int h_place(int n) { return (n & ~127) | ((n >> 3) & 3) << 5 | ((n >> 5) & 3) << 3 | (n & 7); }
-
-// 16 bytes of scales, as they are loaded: from p, or from the last 16 of the matrix if p is nearer to its end.  No branch, so
-// that nothing waits for the load before place() does.  Scales of blocks past a row's end are those of the next row: their
-// lanes have codes of 0 and take a scale of 1.
-struct ScalePiece {
-    u32x4 v;
-    int late;                // bytes that p lies behind where the load began
-    __device__ __forceinline__ void load(const uint8_t *p, const uint8_t *end)
-    {
-        const long long over = p + 16 - end;
-        late = over > 0 ? (int)(over < 16 ? over : 16) : 0;
-        v = ldg<u32x4_any>(over > 0 ? end - 16 : p);
-    }
-    __device__ __forceinline__ void place(char *lds) const
-    {
-        u32x4 r = v;
-        if (__ballot(late > 0)) {
-            const int d = late >> 2, b = late & 3;
-            const uint32_t x[8] = {v.x, v.y, v.z, v.w, 0, 0, 0, 0};
-            uint32_t y[5];
-#pragma unroll
-            for (int i = 0; i < 5; ++i) y[i] = d == 0 ? x[i] : d == 1 ? x[i + 1] : d == 2 ? x[i + 2] : i + 3 < 8 && d == 3 ? x[i + 3] : 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_alignbyte(y[i + 1], y[i], b);
-        }
-        *reinterpret_cast<u32x4 *>(lds) = r;
-    }
-};
 
 // The neurons of a call's live branches (on, and some token of the workgroup's takes them).  Mostly they are one range that the
 // host knows (kOneRun: no routing, one run of active branches); a workgroup then asks for weights at once, without having seen
@@ -227,25 +198,33 @@ __device__ __forceinline__ void gated(const BranchLanes &br, const BranchTable &
 }
 
 // The down projection reads H by whole steps of 128 neurons.  Groups of G that a live branch reaches into are written whole;
-// here the rest of such a step is set to zero.  wave of nw: the work is shared out.
+// here the rest of such a step is set to zero, and all of the branches that only other tokens of a down projection's workgroup
+// take (wide, which has live in it).  wave of nw: the work is shared out.
 __device__ __forceinline__ void clear_range(uint16_t *H, int ldh, int nt, int from, int to, int wave, int nw)
 {
     for (int t = wave; t < nt; t += nw)
-        for (int n = from + (threadIdx.x & 63); n < to; n += 64) H[(size_t)t * ldh + h_place(n)] = 0;
+        for (int p = from / 8 * 8 + (threadIdx.x & 63) * 8; p < to; p += 512) {
+            uint16_t *h = H + (size_t)t * ldh + h_place(p);
+            if (p >= from && p + 8 <= to)
+                *reinterpret_cast<u32x4 *>(h) = u32x4{0, 0, 0, 0};
+            else
+                for (int e = 0; e < 8; ++e)
+                    if (p + e >= from && p + e < to) h[e] = 0;
+        }
 }
 __device__ __forceinline__ void clear_edges(const Range &run, uint16_t *H, int ldh, int nt, int wave, int nw)
 {
     if (run.beg % kStepK) clear_range(H, ldh, nt, run.beg / kStepK * kStepK, run.beg, wave, nw);
     if (run.end % kStepK) clear_range(H, ldh, nt, run.end, (run.end + kStepK - 1) / kStepK * kStepK, wave, nw);
 }
-__device__ __forceinline__ void clear_edges(const OffsetLanes &off, int B, unsigned long long live, uint16_t *H, int ldh, int nt,
-                                            int wave, int nw)
+__device__ __forceinline__ void clear_edges(const OffsetLanes &off, int B, unsigned long long live, unsigned long long wide,
+                                            uint16_t *H, int ldh, int nt, int wave, int nw)
 {
     for (int b = 0; b <= B; ++b) {                       // past the last branch: the rest of its step
         const int from = b < B ? off.first(b) : off.past(B - 1), to = b < B ? off.past(b) : ldh;
         if ((b < B && ((live >> b) & 1)) || to == from) continue;
         const int up = (from + kStepK - 1) / kStepK * kStepK, down = to / kStepK * kStepK;
-        const int end = up < to ? up : to, beg = down > end ? down : end;
+        const int end = up < to && !(b < B && ((wide >> b) & 1)) ? up : to, beg = down > end ? down : end;
         clear_range(H, ldh, nt, from, end, wave, nw);
         clear_range(H, ldh, nt, beg, to, wave, nw);
     }

@@ -190,6 +190,20 @@ def test_routed(mm, T, widths):
     assert not out.any()
 
 
+@pytest.mark.parametrize("T,run_length,d_model,widths", [
+    (T, n, d, w) for T, n in [(16, 5), (40, 9), (64, 32), (64, 10), (300, 20), (300, 48)]
+    for d, w in [(224, [100, 28, 33, 95, 256, 128, 64, 64]), (1024, [512] * 8)]
+] + [(16, 5, 51200, [128] * 4), (40, 9, 51200, [128] * 4)])
+def test_routed_by_sequences(mm, T, run_length, d_model, widths):
+    """Neighbouring tokens take the same branches, other runs of tokens others: a branch that part of a workgroup's tokens take
+    is there for the rest, whose values in the workspace are nobody's."""
+    B = len(widths)
+    r = np.zeros((T, B), np.uint8)
+    for i, t in enumerate(range(0, T, run_length)):
+        r[t:t + run_length, [(2 * i) % B, (2 * i + 1) % B]] = 1
+    check(mm, T, d_model, widths, seed=T + run_length, route=r)
+
+
 @pytest.mark.parametrize("T", [1, 20, 150])
 def test_nothing_active_and_no_tokens(mm, T):
     import torch
