@@ -367,7 +367,8 @@ MLPMOE_API int mlpmoe_forward_routed_f32_ws(const float *x, const float *W_gate,
  * over the blocks, in an order that follows from T and B: results are the same bits from run to run.  No output may overlap
  * an input.  T >= 0 (T == 0: counts and loss are set to zero), T <= 2^24, 1 <= B <= MLPMOE_MAX_BRANCHES.
  * Workspace as for mlpmoe_forward_bf16: mlpmoe_set_workspace()'s block or the library's own; the _ws form takes the caller's,
- * 256-byte aligned, of mlpmoe_route_workspace_bytes(T, B) bytes (0 for invalid sizes), scratch.
+ * 256-byte aligned, of mlpmoe_route_workspace_bytes(T, B) bytes (0 for invalid sizes; what serves T tokens serves fewer),
+ * scratch.
  * Errors: NULL, SHAPE, UNSUPPORTED (elem_bytes), ALIGN, WORKSPACE, HIP.
  */
 MLPMOE_API size_t mlpmoe_route_workspace_bytes(int T, int B);
@@ -417,15 +418,16 @@ MLPMOE_API int mlpmoe_w4_dequantize(const uint8_t *codes, const uint8_t *scales,
  * mlpmoe_forward_w4 / _ws -- the bf16 forward, plain or routed, on 4-bit weights: W_gate and W_up [d_inter, d_model], W_down
  * [d_model, d_inter] as codes and scales each.  x, branch_offsets, alpha, active_mask, T, d_model, d_inter and B as for
  * mlpmoe_forward_bf16; route as for mlpmoe_forward_routed_bf16, or NULL: every token takes every active branch.  d_model and
- * d_inter are multiples of 32 (MLPMOE_ERR_UNSUPPORTED otherwise; mlpmoe_slice_rows makes row counts of compacted layers so),
- * branch boundaries may lie anywhere.
+ * d_inter are multiples of 32 and at most 131072 (MLPMOE_ERR_UNSUPPORTED otherwise; mlpmoe_slice_rows makes row counts of
+ * compacted layers multiples), branch boundaries may lie anywhere.
  *
  * Arithmetic: that of mlpmoe_forward_bf16 on the dequantised weights, h rounded once to bf16, sums in float; out is float
  * (out_bytes 4) or the sums rounded once to bf16 (2), [T, d_model].  It may overlap x.  Results are the same bits from run to
  * run.  An inactive branch, and one that no token takes, contributes nothing: no value of its weights reaches out, unless a block of
  * W_down that it shares with a neighbour has the scale 255.
  *
- * Workspace as for mlpmoe_forward_bf16; mlpmoe_w4_workspace_bytes() bytes (0 for invalid sizes) for the _ws form.
+ * Workspace as for mlpmoe_forward_bf16; mlpmoe_w4_workspace_bytes() bytes (0 for invalid sizes; what serves T tokens serves fewer)
+ * for the _ws form.
  * Errors: those of mlpmoe_forward_bf16, and UNSUPPORTED; T above 1048560 is MLPMOE_ERR_SHAPE.
  */
 MLPMOE_API size_t mlpmoe_w4_workspace_bytes(int T, int d_model, int d_inter, int B);

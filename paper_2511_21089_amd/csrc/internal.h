@@ -163,6 +163,7 @@ struct RouteBackArgs {
     hipStream_t stream;
 };
 int route_blocks(int T, int B);
+int route_most_blocks(int T, int B);              // of any call of up to T tokens
 hipError_t launch_route_topk(const RouteArgs &a);
 hipError_t launch_route_backward(const RouteBackArgs &a);
 
@@ -180,7 +181,7 @@ struct W4Args {
     float *partial;                   // partial sums of a K split of the down projection
     hipStream_t stream;
 };
-int w4_splits(int T, int d_model, int d_inter);
+size_t w4_partial_floats(int T, int d_model, int d_inter);
 hipError_t launch_w4_tiles(const W4Args &a, const BranchTable &bt);
 hipError_t launch_w4_quantize(const void *W, size_t n, int elem_bytes, uint8_t *codes, uint8_t *scales, hipStream_t s);
 hipError_t launch_w4_dequantize(const uint8_t *codes, const uint8_t *scales, size_t n, int elem_bytes, void *W, hipStream_t s);

@@ -453,6 +453,12 @@ hipError_t back_lanes(const RouteBackArgs &a)
 
 }  // namespace
 
+int route_most_blocks(int T, int B)
+{
+    const long long all = (long long)T * lanes(B), want = (all + 255) / 256;
+    return (int)(all <= 2 * kRouteThreads ? 1 : want < kRouteMaxBlocks ? want : kRouteMaxBlocks);
+}
+
 int route_blocks(int T, int B)
 {
     const long long all = (long long)T * lanes(B);

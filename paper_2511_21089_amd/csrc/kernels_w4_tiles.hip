@@ -14,7 +14,7 @@
 namespace mlpmoe {
 namespace {
 
-constexpr int kCus = 256;
+constexpr int kCus = 256, kMostSplits = 8;
 constexpr int kScaleBuf = 1280;          // scales of a wave's rows for 512 of K: 16 bytes a row, or 20 in five loads of a dword
 
 constexpr int stage_bytes(int NA, int NF, int KW, int WR) { return KW * NF * 4096 + KW * WR * NA * 1024; }
@@ -401,11 +401,17 @@ DownTile down_tile(int T, int d_model, int d_inter)
     DownTile t = T <= 32 ? DownTile{0, 128, 32, 1} : T <= 48 ? DownTile{1, 128, 48, 1} : T <= 64 ? DownTile{2, 128, 64, 1} : DownTile{3, 128, 64, 1};
     if (T > 64 && d_model >= 1024 && (long long)ceil_div(d_model, 256) * ceil_div(T, 64) >= 64) t = DownTile{4, 256, 64, 1};
     const long long tiles = (long long)ceil_div(d_model, t.rows) * ceil_div(T, t.tokens);
-    while (t.splits < 8 && tiles * t.splits * 2 <= 512 && d_inter >= kStepK * 8 * t.splits) t.splits *= 2;
+    while (t.splits < kMostSplits && tiles * t.splits * 2 <= 2 * kCus && d_inter >= kStepK * 8 * t.splits) t.splits *= 2;
     return t;
 }
 
-int w4_splits(int T, int d_model, int d_inter) { return down_tile(T, d_model, d_inter).splits; }
+// Room for the partial sums of any call of up to T tokens: at most kMostSplits ranges, and a split leaves at most 2 kCus tiles of 256 x 64.
+size_t w4_partial_floats(int T, int d_model, int d_inter)
+{
+    if (T <= 16 || d_inter < kStepK * 8) return 0;
+    const size_t few = (size_t)kMostSplits * T * d_model, many = (size_t)2 * kCus * 256 * 64;
+    return few < many ? few : many;
+}
 
 // Tiles of gate+up, neurons x tokens: the smallest of 64 x 32, 48 or 64 in two sets of waves with which a workgroup on every CU
 // does it in one go; past that 256 x 128 (8 waves, for a K worth its start) where its rounds over the chip are three quarters

@@ -89,7 +89,7 @@ extern "C" {
 size_t mlpmoe_route_workspace_bytes(int T, int B)
 {
     if (T < 0 || T > (1 << 24) || B < 1 || B > MLPMOE_MAX_BRANCHES) return 0;
-    const int blocks = route_blocks(T, B);
+    const int blocks = route_most_blocks(T, B);
     return part_bytes(blocks, B) + align_up((size_t)blocks * sizeof(int), 256);
 }
 

@@ -98,8 +98,7 @@ int mlpmoe_w4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, 
 size_t mlpmoe_w4_workspace_bytes(int T, int d_model, int d_inter, int B)
 {
     if (T < 0 || d_model < 1 || d_inter < 0 || B < 1 || B > MLPMOE_MAX_BRANCHES) return 0;
-    const int splits = T > 16 ? w4_splits(T, d_model, d_inter) : 1;
-    return h_bytes(T, d_inter) + (splits > 1 ? align_up((size_t)splits * T * d_model * 4, 256) : 0) + 256;
+    return h_bytes(T, d_inter) + align_up(w4_partial_floats(T, d_model, d_inter) * 4, 256) + 256;
 }
 
 int mlpmoe_forward_w4(const void *x, const uint8_t *gate_codes, const uint8_t *gate_scales, const uint8_t *up_codes,

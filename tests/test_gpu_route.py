@@ -156,6 +156,17 @@ def test_far_rows(mm):
     check(mm, big[:, :B], host, 3)
 
 
+@pytest.mark.parametrize("T,B,k", [(1024, 8, 2), (1025, 8, 3), (100003, 64, 6), (600001, 3, 1)])
+def test_many_tokens_a_lane(mm, T, B, k):
+    """A lane with more than one token, with sums and without, the last of them missing here and there; most tokens padding."""
+    import torch
+    x, host = logits_of(T, T, B, torch.float32, banned=0.1)
+    real = (np.random.default_rng(T).uniform(size=T) < 0.4).astype(np.uint8)
+    route, probs, *_ = check(mm, x, host, k, None, real)
+    r, p, *_ = mm.mlpmoe_route_topk(x, k, None, torch.from_numpy(real).cuda(), want_stats=False)
+    assert torch.equal(r, route) and torch.equal(p, probs)
+
+
 def test_forms_agree_and_repeat(mm):
     """Without sums, without probabilities, with a workspace of the caller's: the same route; every run the same bits."""
     import torch

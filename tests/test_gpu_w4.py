@@ -204,6 +204,30 @@ def test_routed_by_sequences(mm, T, run_length, d_model, widths):
     check(mm, T, d_model, widths, seed=T + run_length, route=r)
 
 
+@pytest.mark.parametrize("kind", ["one run", "some off", "routed"])
+@pytest.mark.parametrize("T,d_model,widths", [(300, 96, [256] * 8), (400, 96, [500, 512, 524, 512]), (600, 160, [256] * 8), (1100, 96, [2000, 48]),
+                                              (1600, 2048, [1024, 1000, 1048, 1024])])
+def test_many_tokens(mm, T, d_model, widths, kind):
+    """Enough tiles for every shape of them."""
+    B = len(widths)
+    r = None
+    if kind == "routed":
+        r = routes(np.random.default_rng(T), T, B, 1)
+        r[:, 0] = 0
+        r[:T // 3, B - 1] = 1
+    check(mm, T, d_model, widths, seed=T, off_branches=(1,) if kind == "some off" and B > 2 else (), route=r)
+
+
+@pytest.mark.parametrize("T", [1, 3, 8, 16, 17, 45, 65])
+@pytest.mark.parametrize("d_model,widths,gone", [(131072, [64], ()), (131040, [40, 24], ()), (32, [131072], ()), (32, [50000, 40, 81032], (1,)),
+                                                 (64, [131040], ())])
+def test_longest_rows(mm, T, d_model, widths, gone):
+    rng = np.random.default_rng(T)
+    check(mm, T, d_model, widths, seed=T, off_branches=gone)
+    if len(widths) > 1:
+        check(mm, T, d_model, widths, seed=T, off_branches=gone, route=routes(rng, T, len(widths), 1))
+
+
 @pytest.mark.parametrize("T", [1, 20, 150])
 def test_nothing_active_and_no_tokens(mm, T):
     import torch

@@ -106,6 +106,25 @@ def test_w4_workspace_bytes():
     assert f(0, 64, 128, 2) > 0 and f(16, 4096, 14336, 16) >= 16 * 14336 * 2
 
 
+@pytest.mark.parametrize("d_model,d_inter", [(4096, 14336), (896, 4864), (64, 32), (32, 131072), (131072, 1024)])
+def test_a_workspace_for_more_tokens_serves_fewer(d_model, d_inter):
+    tokens = [*range(200), 255, 256, 257, 500, 1000, 1600, 4000, 100000, 65535 * 16]
+    sizes = [mm.mlpmoe_w4_workspace_bytes(T, d_model, d_inter, 8) for T in tokens]
+    assert sizes == sorted(sizes)
+    for B in (1, 5, 64):
+        sizes = [mm.mlpmoe_route_workspace_bytes(T, B) for T in [*tokens, 1 << 24]]
+        assert sizes == sorted(sizes)
+
+
+def test_forward_w4_refuses_longer_rows():
+    f = mm.lib.mlpmoe_forward_w4
+    al, mk = np.ones(1, np.float32), np.ones(1, np.uint8)
+    for d_model, d_inter in ((131072 + 32, 64), (64, 131072 + 32)):
+        off = np.array([0, d_inter], np.int32)
+        assert f(P, P, P, P, P, P, P, off.ctypes.data, al.ctypes.data, mk.ctypes.data, None, 1, d_model, d_inter, 1, 2, P,
+                 None) == mm.ERR_UNSUPPORTED
+
+
 def test_binding_refuses_what_is_not_on_the_gpu_or_has_another_form():
     torch = pytest.importorskip("torch")
     cpu = torch.zeros((4, 8))
