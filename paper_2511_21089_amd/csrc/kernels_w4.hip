@@ -51,7 +51,8 @@ size_t gate_up_lds(int nt, int nw, int S, int K, bool whole)
 }
 
 // Grid (workgroups, tiles of tt tokens).  A wave works out groups of 8 neurons, MFMA rows 0-7 W_gate and 8-15 W_up; wave w of
-// workgroup g the groups w * grid + g and so on, so that what live groups there are is spread over the chip.
+// workgroup g the groups w * grid + g and so on, so that what live groups there are is spread over the chip.  With x whole in
+// LDS (below) and waves left over, as where tokens take few branches, several waves share a group, chunk by chunk of K in turn.
 // 512 of K at a time, the codes (each wave its own) go through LDS, S - 1 stages ahead, and with them x (for the workgroup), which
 // has the waves meet for every stage; XL = 0: x fits LDS whole, and after one meeting every wave goes at its own pace.  A load of codes
 // is 256 bytes of four rows each: 4096 x 14336, gate and up codes alone, 10.2 us, and 11.3 us with 64 bytes of 16 rows.  Row r's 16-byte
@@ -75,7 +76,7 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
     const int blocks = K / 32, chunks = (K + kChunkK - 1) / kChunkK;
     constexpr bool kWhole = XL == 0;
     const int stage = (kWhole ? 0 : nt * kXRow) + nw * 4096;
-    char *all_x = lds + S * stage, *scrap = all_x + (kWhole ? chunks * nt * kXRow : 0), *my_s = scrap + 1024 + wave * scale_bytes(K);
+    char *all_x = lds + S * stage, *scrap = all_x + (kWhole ? chunks * nt * kXRow : 0);
     Groups<8, kOneRun> groups(run);
     if constexpr (kOneRun) {
         if (blockIdx.x == 0) clear_edges(run, H + (size_t)t0 * ldh, ldh, nt, wave, nw);
@@ -83,8 +84,17 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
         const OffsetLanes off(bt);
         const unsigned long long live = live_of_16(bt, route, 0, T);    // of all tokens: the down projection's tiles may be larger
         groups = Groups<8, kOneRun>(off, live);
-        if (blockIdx.x == 0) clear_edges(off, bt.B, live, live, H + (size_t)t0 * ldh, ldh, nt, wave, nw);
+        clear_edges(off, bt.B, live, live, H + (size_t)t0 * ldh, ldh, nt, wave, nw, blockIdx.x, gridDim.x);
     }
+
+    // parts of K that a group's waves take in turn, and this wave's group and part
+    int parts = 1, slot = wave, part = 0;
+    if constexpr (kWhole) {
+        const int own = __popcll(__ballot(lane < nw && (int)blockIdx.x + lane * (int)gridDim.x < groups.total));
+        while ((parts + 1) * own <= nw && parts < chunks) ++parts;
+        for (slot = 0, part = wave; part >= parts; part -= parts) ++slot;
+    }
+    char *my_s = scrap + 1024 + slot * scale_bytes(K);
 
     // lane of a load of x: place 16 s + 4 q + j of the 64 is piece 16 q + 4 s + j
     const int x_piece = ((lane >> 2) & 3) * 16 + (lane >> 4) * 4 + (lane & 3);
@@ -92,14 +102,14 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
     const int xr = (r16 < nt ? r16 : 0) * kXRow + q * 64, cb = (kWhole ? 0 : nt * kXRow) + wave * 4096;
 #pragma unroll 1
     for (int at = blockIdx.x; at < groups.total; at += nw * (int)gridDim.x) {
-        const int idx = at + wave * (int)gridDim.x;
+        const int idx = at + slot * (int)gridDim.x;
         const bool have = idx < groups.total;
         const int n0 = have ? groups(idx) * 8 : 0;
         if (at != (int)blockIdx.x) pipeline_barrier<0>();               // the last group's stages and scales have been read
         const char *xb = reinterpret_cast<const char *>(x + (size_t)t0 * K);
         const uint8_t *gb = gc + (size_t)n0 * (K / 2), *ub = uc + (size_t)n0 * (K / 2);
-        auto issue = [&](int c, char *dst) {             // always PER loads; past the end the last chunk again
-            const int k = c < chunks ? c : chunks - 1;
+        auto issue = [&](int i, char *dst) {             // always PER loads; past the end the last chunk again
+            const int c = part + i * parts, k = c < chunks ? c : chunks - 1;
 #pragma unroll
             for (int n = 0; n < XL; ++n) {
                 const int t = wave + n * nw;
@@ -123,8 +133,8 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
                         const int k = u / nt, t = u - k * nt;
                         dma16(k * 64 + x_piece < K / 8 ? xb + (size_t)t * K * 2 + k * 1024 + x_piece * 16 : zero, all_x + u * kXRow);
                     }
-                stage_scales(gs + (size_t)n0 * blocks, my_s, K / 4, K % 64 == 0, 0, 1);
-                stage_scales(us + (size_t)n0 * blocks, my_s + K / 4, K / 4, K % 64 == 0, 0, 1);
+                stage_scales(gs + (size_t)n0 * blocks, my_s, K / 4, K % 64 == 0, part, parts);
+                stage_scales(us + (size_t)n0 * blocks, my_s + K / 4, K / 4, K % 64 == 0, part, parts);
             }
             keep_order();
         }
@@ -133,12 +143,12 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
         f32x4 acc = {0, 0, 0, 0};
         if (kWhole && at == (int)blockIdx.x) pipeline_barrier<(AHEAD - 1) * PER>();
 #pragma unroll 1
-        for (int c = 0; c < chunks; ++c) {
+        for (int i = 0, c = part; c < chunks; ++i, c += parts) {
             if (kWhole)
                 wait_loads<(AHEAD - 1) * PER>();
             else
                 pipeline_barrier<(AHEAD - 1) * PER>();
-            issue(c + AHEAD, fill);
+            issue(i + AHEAD, fill);
             const char *mx = kWhole ? all_x + c * nt * kXRow : mine;
             const char *sc = my_s + r16 * blocks + c * 16 + q * 4;
             if (have)
@@ -154,6 +164,14 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
             }
             mine = mine + stage == lds + S * stage ? lds : mine + stage;
             fill = fill + stage == lds + S * stage ? lds : fill + stage;
+        }
+        if (kWhole && parts > 1) {                       // the parts' sums, in order; a wave's go where its codes were
+            wait_loads<0>();
+            f32x4 *sums = reinterpret_cast<f32x4 *>(lds + wave * 4096) + lane;
+            if (part > 0) *sums = acc;
+            pipeline_barrier<0>();
+            if (part > 0) continue;
+            for (int p = 1; p < parts; ++p) acc += sums[p * 256];
         }
         if (!have) continue;
         // neurons 4q .. 4q + 3 of token r16: gate in groups q < 2, up in the lanes 32 on
@@ -385,21 +403,23 @@ hipError_t launch_down(const W4Args &a, const BranchTable &bt, const Range &run)
 }
 
 template <bool kOneRun, int XL, int S>
-hipError_t launch_gate_up(const W4Args &a, const BranchTable &bt, const Range &run, int groups, int nw, int tt)
+hipError_t launch_gate_up(const W4Args &a, const BranchTable &bt, const Range &run, int groups, int share, int nw, int tt)
 {
     const size_t lds = gate_up_lds(a.T < tt ? a.T : tt, nw, S, a.d_model, XL == 0);
     const hipError_t e = allow_lds<w4_gate_up<kOneRun, XL, S>>((int)lds, "w4_gate_up attribute");
     if (e != hipSuccess) return e;
     const int resident = 256 * (int)(160 * 1024 / lds);
-    const int grid = ceil_div(groups, nw) < resident ? ceil_div(groups, nw) : resident;
+    const int grid = ceil_div(groups, share) < resident ? ceil_div(groups, share) : resident;
     ProfileScope ps(MLPMOE_KERNEL_W4_GATE_UP, a.stream);
     w4_gate_up<kOneRun, XL, S><<<dim3(grid, ceil_div(a.T, tt)), nw * 64, lds, a.stream>>>(
         static_cast<const uint16_t *>(a.x), a.T, tt, a.d_model, a.gc, a.gs, a.uc, a.us, static_cast<uint16_t *>(a.H), a.ldh, a.route, run, bt);
     return launch_status("w4_gate_up launch");
 }
 
-// A wave a group for every CU's share of the groups, up to 8; three stages, x whole if there is room for it.  (More stages, that
-// is requests in flight, take longer: 4096 x 14336, T = 1: four 18.0 us, three 16.8.)  Where three stages with x in them do not fit,
+// A wave a group for every CU's share of the groups, up to 8; three stages, x whole if there is room for it, and then as many waves as
+// can share the groups, for a routed call 8, since fewer groups than the most are live (us with their events, the waves sharing and not: T = 1, one
+// of 8 or 16 branches, 4096 x 14336 12.8, 16.2; 8192 x 8192 11.8, 19.9, unrouted 20.2, 21.7; 896 x 4864, T = 16, two of 8, 12.0, 15.1).  (More
+// stages, that is requests in flight, take longer: 4096 x 14336, T = 1: four 18.0 us, three 16.8.)  Where three stages with x in them do not fit,
 // up to two waves fewer, then two stages.  A wave loads up to four tokens of x.
 template <bool kOneRun>
 hipError_t gate_up(const W4Args &a, const BranchTable &bt, const Range &run, int groups)
@@ -408,18 +428,21 @@ hipError_t gate_up(const W4Args &a, const BranchTable &bt, const Range &run, int
     auto fits = [&](int nw, int S, bool whole) { return gate_up_lds(nt, nw, S, K, whole) <= (size_t)kLdsBytes; };
     int want = ceil_div(groups, 256);
     want = want > 8 ? 8 : want;
-    if (fits(want, 3, true)) return launch_gate_up<kOneRun, 0, 3>(a, bt, run, groups, want, 16);
+    const int chunks = ceil_div(K, kChunkK), more = want * (8 / want < chunks ? 8 / want : chunks);
+    const int nw = a.route && more < 8 && chunks > 1 ? 8 : more;
+    if (fits(nw, 3, true)) return launch_gate_up<kOneRun, 0, 3>(a, bt, run, groups, want, nw, 16);
+    if (fits(want, 3, true)) return launch_gate_up<kOneRun, 0, 3>(a, bt, run, groups, want, want, 16);
     want = want < least ? least : want;
     for (int n = want; n >= least && n >= want - 2; --n) {
         if (!fits(n, 3, false)) continue;
         const int xl = ceil_div(nt, n);
-        return xl <= 2   ? launch_gate_up<kOneRun, 2, 3>(a, bt, run, groups, n, 16)
-               : xl == 3 ? launch_gate_up<kOneRun, 3, 3>(a, bt, run, groups, n, 16)
-                         : launch_gate_up<kOneRun, 4, 3>(a, bt, run, groups, n, 16);
+        return xl <= 2   ? launch_gate_up<kOneRun, 2, 3>(a, bt, run, groups, n, n, 16)
+               : xl == 3 ? launch_gate_up<kOneRun, 3, 3>(a, bt, run, groups, n, n, 16)
+                         : launch_gate_up<kOneRun, 4, 3>(a, bt, run, groups, n, n, 16);
     }
     for (int n = want; n >= least; --n)
-        if (fits(n, 2, false)) return launch_gate_up<kOneRun, 4, 2>(a, bt, run, groups, n, 16);
-    return launch_gate_up<kOneRun, 4, 2>(a, bt, run, groups, 1, 4);      // scales of a very long K: one wave, four tokens at a time
+        if (fits(n, 2, false)) return launch_gate_up<kOneRun, 4, 2>(a, bt, run, groups, n, n, 16);
+    return launch_gate_up<kOneRun, 4, 2>(a, bt, run, groups, 1, 1, 4);      // scales of a very long K: one wave, four tokens at a time
 }
 
 // 16 waves while three stages of their chunks fit, else 8, whose chunks are half as long.  H whole if it fits for up to 8 tokens, us

@@ -208,7 +208,7 @@ w4_tile_gate_up(const uint16_t *__restrict__ x, int T, int K, int d_inter, const
         const int r0 = t0 / reach * reach, upto = (t0 + nt + reach - 1) / reach * reach, r1 = upto < T ? upto : T;
         const unsigned long long wide = route && (r0 < t0 || r1 > t0 + nt) ? live_of(bt, route, r0, r1 - r0, any + 2) : live;
         groups = Groups<16, kOneRun>(off, live);
-        clear_edges(off, bt.B, live, wide, H + (size_t)t0 * ldh, ldh, nt, row * WR + wave, row_tiles * WR);
+        clear_edges(off, bt.B, live, wide, H + (size_t)t0 * ldh, ldh, nt, wave, WR, row, row_tiles);
         if (row * WR * NR >= groups.total) return;
     }
 
