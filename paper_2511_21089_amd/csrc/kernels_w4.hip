@@ -65,7 +65,7 @@ template <bool kOneRun, int XL, int S>
 __global__ void __launch_bounds__(512)
 w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *__restrict__ gc, const uint8_t *__restrict__ gs,
            const uint8_t *__restrict__ uc, const uint8_t *__restrict__ us, uint16_t *__restrict__ H, int ldh,
-           const uint8_t *__restrict__ route, Range run, BranchTable bt)
+           const uint8_t *__restrict__ route, int parts_if_one, Range run, BranchTable bt)
 {
     constexpr int PER = 4 + XL, AHEAD = S - 1;
     static_assert((AHEAD - 1) * PER < 63, "loads in flight");
@@ -88,12 +88,13 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
     }
 
     // parts of K that a group's waves take in turn, and this wave's group and part
-    int parts = 1, slot = wave, part = 0;
-    if constexpr (kWhole) {
+    int parts = kWhole && kOneRun ? parts_if_one : 1, slot = wave, part = 0;
+    if constexpr (kWhole && !kOneRun) {
         const int own = __popcll(__ballot(lane < nw && (int)blockIdx.x + lane * (int)gridDim.x < groups.total));
-        while ((parts + 1) * own <= nw && parts < chunks) ++parts;
-        for (slot = 0, part = wave; part >= parts; part -= parts) ++slot;
+        while (own > 0 && (parts + 1) * own <= nw && parts < chunks) ++parts;
     }
+    if (kWhole && parts > 1)
+        for (slot = 0, part = wave; part >= parts; part -= parts) ++slot;
     char *my_s = scrap + 1024 + slot * scale_bytes(K);
 
     // lane of a load of x: place 16 s + 4 q + j of the 64 is piece 16 q + 4 s + j
@@ -412,14 +413,16 @@ hipError_t launch_gate_up(const W4Args &a, const BranchTable &bt, const Range &r
     const int grid = ceil_div(groups, share) < resident ? ceil_div(groups, share) : resident;
     ProfileScope ps(MLPMOE_KERNEL_W4_GATE_UP, a.stream);
     w4_gate_up<kOneRun, XL, S><<<dim3(grid, ceil_div(a.T, tt)), nw * 64, lds, a.stream>>>(
-        static_cast<const uint16_t *>(a.x), a.T, tt, a.d_model, a.gc, a.gs, a.uc, a.us, static_cast<uint16_t *>(a.H), a.ldh, a.route, run, bt);
+        static_cast<const uint16_t *>(a.x), a.T, tt, a.d_model, a.gc, a.gs, a.uc, a.us, static_cast<uint16_t *>(a.H), a.ldh, a.route,
+        nw / share, run, bt);
     return launch_status("w4_gate_up launch");
 }
 
-// A wave a group for every CU's share of the groups, up to 8; three stages, x whole if there is room for it, and then as many waves as
-// can share the groups, for a routed call 8, since fewer groups than the most are live (us with their events, the waves sharing and not: T = 1, one
-// of 8 or 16 branches, 4096 x 14336 12.8, 16.2; 8192 x 8192 11.8, 19.9, unrouted 20.2, 21.7; 896 x 4864, T = 16, two of 8, 12.0, 15.1).  (More
-// stages, that is requests in flight, take longer: 4096 x 14336, T = 1: four 18.0 us, three 16.8.)  Where three stages with x in them do not fit,
+// A wave a group for every CU's share of the groups, up to 8; three stages, x whole if there is room for it.  Then waves can share
+// groups: in a routed call as many as there are to spare, the most being 8 (which groups are live, the kernel sees); in another
+// one from 8 chunks of K on.  us with their events, shared and not: T = 1 on one of 8 or 16 branches 4096 x 14336 12.8, 16.2, 8192 x 8192 11.8,
+// 19.9; T = 1 unrouted 6144 x 2048 8.8, 14.8, 4096 x 4096 10.0, 11.8, 8192 x 8192 20.3, 21.6, but 2048 x 7168 9.2, 8.9.  (More stages, that
+// is requests in flight, take longer: 4096 x 14336, T = 1: four 18.0 us, three 16.8.)  Where three stages with x in them do not fit,
 // up to two waves fewer, then two stages.  A wave loads up to four tokens of x.
 template <bool kOneRun>
 hipError_t gate_up(const W4Args &a, const BranchTable &bt, const Range &run, int groups)
@@ -428,8 +431,8 @@ hipError_t gate_up(const W4Args &a, const BranchTable &bt, const Range &run, int
     auto fits = [&](int nw, int S, bool whole) { return gate_up_lds(nt, nw, S, K, whole) <= (size_t)kLdsBytes; };
     int want = ceil_div(groups, 256);
     want = want > 8 ? 8 : want;
-    const int chunks = ceil_div(K, kChunkK), more = want * (8 / want < chunks ? 8 / want : chunks);
-    const int nw = a.route && more < 8 && chunks > 1 ? 8 : more;
+    const int chunks = ceil_div(K, kChunkK);
+    const int nw = kOneRun ? (chunks < 8 ? want : want * (8 / want)) : chunks > 1 ? 8 : want;
     if (fits(nw, 3, true)) return launch_gate_up<kOneRun, 0, 3>(a, bt, run, groups, want, nw, 16);
     if (fits(want, 3, true)) return launch_gate_up<kOneRun, 0, 3>(a, bt, run, groups, want, want, 16);
     want = want < least ? least : want;
