@@ -167,6 +167,26 @@ def test_many_tokens_a_lane(mm, T, B, k):
     assert torch.equal(r, route) and torch.equal(p, probs)
 
 
+def test_most_tokens(mm):
+    """2^24 tokens, every count exact and the loss within its bound (the sums of a lane's and a block's tokens in float)."""
+    import torch
+    T, B = 1 << 24, 4
+    x = torch.randn((T, B), generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").to(torch.bfloat16)
+    route, probs, counts, loss = mm.mlpmoe_route_topk(x, 1)
+    best = x.float().amax(dim=1, keepdim=True)
+    want = x.float() == best
+    for b in range(1, B):
+        want[:, b] &= ~want[:, :b].any(dim=1)                     # the lowest of equal ones
+    want = want.to(torch.uint8)
+    assert torch.equal(route, want)
+    assert torch.equal(counts[:B], want.sum(dim=0, dtype=torch.int32)) and int(counts[B]) == T
+    p = torch.softmax(x.double(), dim=1)
+    assert float((probs.double() - p).abs().max()) <= U * (3 * 2 * 12 + B + 8)
+    exact = float(B * (want.double().mean(dim=0) * p.mean(dim=0)).sum())
+    rel = U * (3 * 2 * 12 + B + 8 + T / 256 / 1024 + 1024)         # additions of a lane, then of its block
+    assert abs(float(loss) - exact) <= rel * exact
+
+
 def test_forms_agree_and_repeat(mm):
     """Without sums, without probabilities, with a workspace of the caller's: the same route; every run the same bits."""
     import torch

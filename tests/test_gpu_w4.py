@@ -83,6 +83,18 @@ def test_conversion_of_many(mm):
     assert none[0].shape == (0, 1024) and mm.mlpmoe_w4_dequantize(*none).shape == (0, 2048)
 
 
+def test_conversion_past_32_bits(mm):
+    import torch
+    W = torch.zeros((70000, 32768), dtype=torch.bfloat16, device="cuda")
+    W[-3:] = torch.randn((3, 32768), generator=torch.Generator().manual_seed(1)).cuda().to(torch.bfloat16)
+    codes, scales = mm.mlpmoe_w4_quantize(W)
+    o = w4.quantize(W[-4:].double().cpu().numpy())
+    assert np.array_equal(codes[-4:].cpu().numpy(), o[0]) and np.array_equal(scales[-4:].cpu().numpy(), o[1])
+    assert not codes[:-3].any()
+    V = mm.mlpmoe_w4_dequantize(codes, scales, out=W)
+    assert np.array_equal(V[-4:].double().cpu().numpy(), w4.dequantize(codes[-4:].cpu().numpy(), scales[-4:].cpu().numpy()))
+
+
 # ------------------------------------------------------------------------------------------------ forward
 def layer(mm, T, d_model, widths, seed, scale=0.02):
     """x as bf16 bits, packed weights on the GPU, their values as float32, offsets, alpha."""
@@ -226,6 +238,44 @@ def test_longest_rows(mm, T, d_model, widths, gone):
     check(mm, T, d_model, widths, seed=T, off_branches=gone)
     if len(widths) > 1:
         check(mm, T, d_model, widths, seed=T, off_branches=gone, route=routes(rng, T, len(widths), 1))
+
+
+@pytest.mark.parametrize("T", [1, 9, 40])
+def test_weights_past_32_bits(mm, T):
+    """The largest matrices, 8 GiB of codes each, zero but for the last neurons: the layer that has only these.  The sums over
+    d_model may be in another order, so an h may be rounded the other way: 2^-8 of it, and of the result."""
+    import torch
+    n, some = 131072, 96
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn((T, n), generator=g, device="cuda").to(torch.bfloat16)
+    far, near = [], []
+    for rows, cols in ((n, n), (n, n), (n, n)):
+        codes = torch.zeros((rows, cols // 2), dtype=torch.uint8, device="cuda")
+        scales = torch.full((rows, cols // 32), 118, dtype=torch.uint8, device="cuda")
+        where = (slice(n - some, n), slice(None)) if len(far) < 2 else (slice(None), slice((n - some) // 2, n // 2))
+        codes[where] = torch.randint(256, codes[where].shape, generator=g, dtype=torch.uint8, device="cuda")
+        far.append((codes, scales))
+        part = scales[where] if len(far) < 3 else scales[:, (n - some) // 32:]
+        near.append((codes[where].contiguous(), part.contiguous()))
+    al, mk = np.ones(1, np.float32), np.ones(1, np.uint8)
+    got = mm.mlpmoe_forward_w4(x, *far, np.array([0, n], np.int32), al, mk, out_dtype=torch.float32)
+    want = mm.mlpmoe_forward_w4(x, *near, np.array([0, some], np.int32), al, mk, out_dtype=torch.float32).double()
+    rms = want.square().mean().sqrt()
+    assert rms > 0 and float((got.double() - want).abs().max()) <= 1e-2 * float(rms)
+
+
+def test_most_tokens(mm):
+    """As many tokens as a call takes, 999 of them again and again: the same bits wherever they stand."""
+    import torch
+    T, n = 65535 * 16, 999
+    x, packed, values, off, alpha = layer(mm, n, 64, [40, 24], seed=8)
+    mask = np.ones(2, np.uint8)
+    small, _ = run(mm, x, packed, off, alpha, mask)
+    xs = mm.bf16_tensor(x).repeat(T // n + 1, 1)[:T].contiguous()
+    out = mm.mlpmoe_forward_w4(xs, *packed, off, alpha, mask, out_dtype=torch.float32)
+    first = out[:n]
+    assert torch.equal(out, first.repeat(T // n + 1, 1)[:T])
+    assert float((first - small).abs().max()) <= 1e-2 * float(small.square().mean().sqrt())
 
 
 @pytest.mark.parametrize("T", [1, 20, 150])
