@@ -425,8 +425,8 @@ def _bytes_mask(mask, n, what):
 
 
 def _out(t, shape, dtype, device, what):
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+    if t is None:                            # torch.empty takes 1.6 us here, torch.empty_strided 1.25
+        return torch.empty_strided(shape, (shape[1], 1), dtype=dtype, device=device)
     if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of %s" % (what, list(shape), dtype))
     return t
@@ -464,8 +464,8 @@ def mlpmoe_route_topk(logits, k, active_mask=None, token_mask=None, route=None, 
     route = _out(route, (T, B), torch.uint8, dev, "route")
     if want_probs or probs is not None:
         probs = _out(probs, (T, B), torch.float32, dev, "probs")
-    counts = torch.empty(B + 1, dtype=torch.int32, device=dev) if want_stats else None
-    loss = torch.empty(1, dtype=torch.float32, device=dev) if want_stats else None
+    counts = torch.empty_strided((B + 1,), (1,), dtype=torch.int32, device=dev) if want_stats else None
+    loss = torch.empty_strided((1,), (1,), dtype=torch.float32, device=dev) if want_stats else None
     ptrs = _here(token_mask, route, probs, counts, loss, workspace)
     if logits.get_device() != _current_device():
         raise ValueError("expected GPU tensors on the current device")
@@ -518,6 +518,11 @@ def _w4_shape(codes, scales):
     return rows, cols
 
 
+def _w4_fits(codes, scales, rows, cols):
+    return (codes.dtype == torch.uint8 and scales.dtype == torch.uint8 and codes.shape == (rows, cols // 2) and
+            scales.shape == (rows, cols // 32) and cols % 2 == 0)
+
+
 def mlpmoe_w4_dequantize(codes, scales, dtype=None, out=None, stream=None):
     """The values of 4-bit weights, in bf16 (exact) or float32."""
     rows, cols = _w4_shape(codes, scales)
@@ -544,8 +549,9 @@ def mlpmoe_forward_w4(x, gate, up, down, branch_offsets, alpha, active_mask, rou
     d_inter = int(off[-1])
     if x.dtype != torch.bfloat16:
         raise ValueError("x must be bfloat16")
-    if _w4_shape(*gate) != (d_inter, d_model) or _w4_shape(*up) != (d_inter, d_model) or _w4_shape(*down) != (d_model, d_inter):
-        raise ValueError("weights do not fit x and branch_offsets")
+    if not (_w4_fits(*gate, d_inter, d_model) and _w4_fits(*up, d_inter, d_model) and _w4_fits(*down, d_model, d_inter)):
+        raise ValueError("4-bit weights are codes [rows, cols / 2] and scales [rows, cols / 32], both uint8, and these do not fit x "
+                         "and branch_offsets")
     if route is not None and (route.dtype != torch.uint8 or tuple(route.shape) != (T, B)):
         raise ValueError("route must be a [T, B] uint8 tensor")
     if out_dtype is None:
