@@ -184,7 +184,7 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
             br, bt, n0, n0 + 4 * (q & 1), acc, up,
             [&](int b) { return kOneRun || !route || (r16 < nt && route[(size_t)(t0 + r16) * bt.B + b] != 0); },
             [&](uint2 h) {
-                if (q < 2 && r16 < nt) *reinterpret_cast<uint2 *>(H + (size_t)(t0 + r16) * ldh + h_place(n0 + 4 * q)) = h;
+                if (q < 2 && r16 < nt) *reinterpret_cast<uint2 *>(H + (size_t)(t0 + r16) * ldh + n0 + 4 * q) = h;
             });
     }
     pipeline_barrier<0>();                               // loads past the end are still on their way into LDS
@@ -203,7 +203,8 @@ size_t down_lds(int W, int S, int nt, int K, bool one, bool whole)
 // steps of K each wave has one, so that together the waves read W * 64 bytes of a row.  Codes (each wave its own) and H (for the
 // workgroup) go through LDS, S - 1 chunks ahead, and the waves meet for every chunk; NL = 0: H of up to 16 tokens lies in LDS whole, and
 // after one meeting every wave goes at its own pace.  A step is live if a live branch has a neuron in it; the others are left out.  The waves' sums are added in
-// their order.  4096 x 14336: T = 1 7.9 us (31 MB, 3.9 TB/s), T = 16 14.5, bound by H, which every workgroup reads (117 MB out of L2).
+// their order.  4096 x 14336: T = 1 7.9 us (31 MB, 3.9 TB/s), T = 16 13.9, bound by H, which every workgroup reads (117 MB out of L2;
+// four waves more that only load H, so that codes can be asked for five chunks ahead, do not help: 14.3).
 // Asking for the codes at the end of the kernel before does not help: with all of them in L2 this one takes 7.6 us instead
 // of 8.4 (H by chunks), and that one longer by more.
 template <bool kOneRun, int W, int NL, int S>
@@ -235,8 +236,7 @@ w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__
     }
     const uint8_t *codes = dc + (size_t)(m0 + r16) * (K / 2);
     const char *hb = reinterpret_cast<const char *>(H + (size_t)t0 * ldh);
-    // this lane's piece of a load of H: step lane >> 4 of four, piece (4 q + j) of it from place 4 j + q
-    const int h_lane = ((lane & 3) << 2 | ((lane >> 2) & 3)) * 16;
+    const int h_lane = r16 * 16;                         // a load of H: four steps, piece r16 of step q
     const int q_last = (q < blocks - (all - 1) * 4 ? q : 0) * 16;
     auto step_of = [&](int i) { return i < steps ? (kOneRun ? s_beg + i : (int)list[i]) : -1; };
     auto issue = [&](int c, char *dst) {                 // always PER loads

@@ -28,11 +28,10 @@ constexpr int core_lds(int NA, int NF, int AHEAD, int KW, int WR)
 }
 
 // acc[a][f] += 16 rows (codes[a], this wave's) x 16 tokens over the n > 0 steps step(0) .. step(n - 1), ascending (past the end
-// the last one).  srow:
-// this lane's row of scales, lane 16 a + r for row r of codes[a]; send: their end.  on(b): whether block b is read (the scale of
-// another may be no number; x is zero there).  The sum is in the first set's waves.  kPlaced: X is H, whose pieces lie in the
-// order in which they are read, rows of whole steps; else a row is K long.
-template <int NA, int NF, int AHEAD, int KW, int WR, bool kPlaced, typename StepOf, typename On>
+// the last one).  srow: this lane's row of scales, lane 16 a + r for row r of codes[a]; send: their end.  on(b): whether block b is read (the scale of
+// another may be no number; x is zero there).  The sum is in the first set's waves.  kWholeSteps: X is H, whose rows are
+// whole steps; else a row is K long.
+template <int NA, int NF, int AHEAD, int KW, int WR, bool kWholeSteps, typename StepOf, typename On>
 __device__ __forceinline__ void sum_steps(f32x4 (&acc)[NA][NF], const uint8_t *const (&codes)[NA], const uint8_t *srow,
                                           const uint8_t *send, const uint16_t *__restrict__ X, int ldx, int last_token, int K,
                                           char *lds, int n, StepOf step_of, On on)
@@ -49,7 +48,7 @@ __device__ __forceinline__ void sum_steps(f32x4 (&acc)[NA][NF], const uint8_t *c
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
         const int unit = wave * NX + i, t = unit % (NF * 4) * 4 + q, c = r16 ^ (t & 15);
-        x_off[i] = (unsigned)((t < last_token ? t : last_token) * ldx * 2 + (kPlaced ? (c & 3) * 4 + c / 4 : c) * 16);
+        x_off[i] = (unsigned)((t < last_token ? t : last_token) * ldx * 2 + c * 16);
         x_k[i] = c * 8;
     }
     const int w_row = r16 * (K / 2);
@@ -78,7 +77,7 @@ __device__ __forceinline__ void sum_steps(f32x4 (&acc)[NA][NF], const uint8_t *c
         for (int j = 0; j < NX; ++j) {
             const int u = KW == 1 ? s : step_of(i * KW + (wave * NX + j) / (NF * 4));
             const char *src = xb + (size_t)u * 256 + x_off[j];
-            if (!kPlaced && u == all - 1) src = u * kStepK + x_k[j] < K ? src : zero;
+            if (!kWholeSteps && u == all - 1) src = u * kStepK + x_k[j] < K ? src : zero;
             dma16(src, dst + (wave * NX + j) * 1024);
         }
         const int off = w_row + s * 64 + (s == all - 1 ? q_last : q) * 16;
@@ -249,7 +248,7 @@ w4_tile_gate_up(const uint16_t *__restrict__ x, int T, int K, int d_inter, const
                 br, bt, n0, n0 + 4 * q, g, u,
                 [&](int b) { return kOneRun || !route || (t < nt && route[(size_t)(t0 + t) * bt.B + b] != 0); },
                 [&](uint2 h) {
-                    if (t < nt) *reinterpret_cast<uint2 *>(H + (size_t)(t0 + t) * ldh + h_place(n0 + 4 * q)) = h;
+                    if (t < nt) *reinterpret_cast<uint2 *>(H + (size_t)(t0 + t) * ldh + n0 + 4 * q) = h;
                 });
         }
     });

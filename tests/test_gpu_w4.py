@@ -120,10 +120,9 @@ def run(mm, x, packed, off, alpha, mask, route=None, out_dtype=None):
     r = None if route is None else torch.from_numpy(route).cuda()
     mm.mlpmoe_forward_w4(mm.bf16_tensor(x), *packed, off, alpha, mask, route=r, out=out, workspace=ws)
     torch.cuda.synchronize()
-    # H: rows of whole 128s, in each of which the 8-neuron pieces 4 q + j lie at 4 j + q
+    # H: rows of whole 128s
     ld = (d_inter + 127) // 128 * 128
-    H = ws[:T * ld * 2].view(torch.int16).view(T, ld // 128, 4, 4, 8).transpose(2, 3).reshape(T, ld)[:, :d_inter]
-    H = H.contiguous().cpu().numpy().view(np.uint16)
+    H = ws[:T * ld * 2].view(torch.int16).view(T, ld)[:, :d_inter].contiguous().cpu().numpy().view(np.uint16)
     return out, synth.bf16_bits_to_f32(H).astype(np.float64)
 
 
