@@ -203,8 +203,8 @@ size_t down_lds(int W, int S, int nt, int K, bool one, bool whole)
 // steps of K each wave has one, so that together the waves read W * 64 bytes of a row.  Codes (each wave its own) and H (for the
 // workgroup) go through LDS, S - 1 chunks ahead, and the waves meet for every chunk; NL = 0: H of up to 16 tokens lies in LDS whole, and
 // after one meeting every wave goes at its own pace.  A step is live if a live branch has a neuron in it; the others are left out.  The waves' sums are added in
-// their order.  4096 x 14336: T = 1 7.9 us (31 MB, 3.9 TB/s), T = 16 13.9, bound by H, which every workgroup reads (117 MB out of L2;
-// four waves more that only load H, so that codes can be asked for five chunks ahead, do not help: 14.3).
+// their order.  4096 x 14336: T = 1 7.5 us (31 MB, 4.1 TB/s), T = 16 12.5, bound by H, which every workgroup reads (117 MB out of L2;
+// four waves more that only load H, so that codes can be asked for five chunks ahead, do not help).
 // Asking for the codes at the end of the kernel before does not help: with all of them in L2 this one takes 7.6 us instead
 // of 8.4 (H by chunks), and that one longer by more.
 template <bool kOneRun, int W, int NL, int S>
@@ -234,10 +234,11 @@ w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__
         mark_blocks(off, live_of_16(bt, route, t0, nt), bits, blocks);
         steps = list_steps(bits, all, list);
     }
-    const uint8_t *codes = dc + (size_t)(m0 + r16) * (K / 2);
+    const CodeLane cl;
+    const uint8_t *codes = dc + (size_t)(m0 + cl.row) * (K / 2);
     const char *hb = reinterpret_cast<const char *>(H + (size_t)t0 * ldh);
     const int h_lane = r16 * 16;                         // a load of H: four steps, piece r16 of step q
-    const int q_last = (q < blocks - (all - 1) * 4 ? q : 0) * 16;
+    const int block_last = (cl.block < blocks - (all - 1) * 4 ? cl.block : 0) * 16;
     auto step_of = [&](int i) { return i < steps ? (kOneRun ? s_beg + i : (int)list[i]) : -1; };
     auto issue = [&](int c, char *dst) {                 // always PER loads
 #pragma unroll
@@ -249,7 +250,7 @@ w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__
                   t < nt ? dst + t * h_row + part * 1024 : scrap);
         }
         const int s = step_of(c * W + wave);
-        dma16(s >= 0 ? reinterpret_cast<const char *>(codes + s * 64 + (s == all - 1 ? q_last : q * 16)) : reinterpret_cast<const char *>(g_zero16),
+        dma16(s >= 0 ? reinterpret_cast<const char *>(codes + s * 64 + (s == all - 1 ? block_last : cl.block * 16)) : reinterpret_cast<const char *>(g_zero16),
               dst + h_stage + wave * 1024);
     };
     const int chunks = (steps + W - 1) / W;
@@ -274,7 +275,7 @@ w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__
     f32x4 acc = {0, 0, 0, 0};
     const char *mine = lds, *end = lds + S * stage;
     char *fill = lds + AHEAD * stage;
-    const int hr = (r16 < nt ? r16 : 0) * h_row + wave * 256 + q * 64, wr = h_stage + wave * 1024 + lane * 16;
+    const int hr = (r16 < nt ? r16 : 0) * h_row + wave * 256 + q * 64, wr = h_stage + wave * 1024 + cl.at;
     if (kWhole) pipeline_barrier<(AHEAD - 1) * PER>();
 #pragma unroll 1
     for (int c = 0; c < chunks; ++c) {

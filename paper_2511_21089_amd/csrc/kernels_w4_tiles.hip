@@ -51,8 +51,9 @@ __device__ __forceinline__ void sum_steps(f32x4 (&acc)[NA][NF], const uint8_t *c
         x_off[i] = (unsigned)((t < last_token ? t : last_token) * ldx * 2 + c * 16);
         x_k[i] = c * 8;
     }
-    const int w_row = r16 * (K / 2);
-    const int q_last = q < blocks - (all - 1) * 4 ? q : 0;              // in the last step there may be fewer blocks than groups of lanes
+    const CodeLane cl;
+    const int w_row = cl.row * (K / 2);
+    const int block_last = cl.block < blocks - (all - 1) * 4 ? cl.block : 0;     // in the last step there may be fewer than four
     const bool by16 = K % 512 == 0;
     const int late = by16 ? 0 : (r16 * blocks) & 3;                     // bytes of a dword before a row's
     char *my_s = lds + (AHEAD + 1) * STAGE + wave * ((AHEAD + 1) * kScaleBuf);
@@ -80,7 +81,7 @@ __device__ __forceinline__ void sum_steps(f32x4 (&acc)[NA][NF], const uint8_t *c
             if (!kWholeSteps && u == all - 1) src = u * kStepK + x_k[j] < K ? src : zero;
             dma16(src, dst + (wave * NX + j) * 1024);
         }
-        const int off = w_row + s * 64 + (s == all - 1 ? q_last : q) * 16;
+        const int off = w_row + s * 64 + (s == all - 1 ? block_last : cl.block) * 16;
 #pragma unroll
         for (int a = 0; a < NA; ++a) dma16(codes[a] + off, dst + w_at + a * 1024);
     };
@@ -113,7 +114,7 @@ __device__ __forceinline__ void sum_steps(f32x4 (&acc)[NA][NF], const uint8_t *c
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
             const uint32_t byte = *reinterpret_cast<const uint8_t *>(sc + a * a_step);
-            w[a] = *reinterpret_cast<const u32x4 *>(mine + w_at + a * 1024 + lane * 16);
+            w[a] = *reinterpret_cast<const u32x4 *>(mine + w_at + a * 1024 + cl.at);
             // the second set has no step where their number is odd: codes of zero
             if (KW > 1 && !mine_too) w[a] = u32x4{0, 0, 0, 0};
             scale[a] = scale_of(live && mine_too ? byte : 127u);

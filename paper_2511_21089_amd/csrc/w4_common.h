@@ -86,6 +86,21 @@ __device__ __forceinline__ uint16_t to_bf16(float v) { return __builtin_bit_cast
 // gather every fourth piece make four requests of one (4096 x 14336: w4_down, T = 16, 14.6 us instead of 13.9, w4_tile_down, T = 24, 14.0 instead of 12.8).
 constexpr int kStepK = 128;
 
+// A load of a step's codes of 16 rows: lane's row and its block of the step, four neighbouring lanes 64 bytes of a row; and where in
+// the kilobyte of LDS that it fills the lane finds row r16, block q, so that 16 lanes read different banks.  (Against lanes that load
+// what they use, neighbours in different rows, 4096 x 14336: w4_down T = 1 7.5 us instead of 7.9, T = 16 12.5 and 13.8; w4_tile_gate_up T = 24
+// 17.9 and 19.8, T = 500 107 and 109.)
+struct CodeLane {
+    int row, block, at;
+    __device__ __forceinline__ CodeLane()
+    {
+        const int lane = threadIdx.x & 63, r16 = lane & 15, q = lane >> 4;
+        row = lane >> 2;
+        block = (lane & 3) ^ (lane >> 4);
+        at = (r16 * 4 + (q ^ (r16 >> 2))) * 16;
+    }
+};
+
 // The neurons of a call's live branches (on, and some token of the workgroup's takes them).  Mostly they are one range that the
 // host knows (kOneRun: no routing, one run of active branches); a workgroup then asks for weights at once, without having seen
 // the table, whose arguments take a round trip.  Otherwise the table and the routes are looked through first, and what comes
