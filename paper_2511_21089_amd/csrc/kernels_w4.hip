@@ -203,7 +203,7 @@ size_t down_lds(int W, int S, int nt, int K, bool one, bool whole)
 // steps of K each wave has one, so that together the waves read W * 64 bytes of a row.  Codes (each wave its own) and H (for the
 // workgroup) go through LDS, S - 1 chunks ahead, and the waves meet for every chunk; NL = 0: H of up to 16 tokens lies in LDS whole, and
 // after one meeting every wave goes at its own pace.  A step is live if a live branch has a neuron in it; the others are left out.  The waves' sums are added in
-// their order.  4096 x 14336: T = 1 7.5 us (31 MB, 4.1 TB/s), T = 16 12.5, bound by H, which every workgroup reads (117 MB out of L2;
+// their order.  4096 x 14336: T = 1 7.5 us (31 MB, 4.1 TB/s), T = 16 12.3, bound by H, which every workgroup reads (117 MB out of L2;
 // four waves more that only load H, so that codes can be asked for five chunks ahead, do not help).
 // Asking for the codes at the end of the kernel before does not help: with all of them in L2 this one takes 7.6 us instead
 // of 8.4 (H by chunks), and that one longer by more.
@@ -234,24 +234,30 @@ w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__
         mark_blocks(off, live_of_16(bt, route, t0, nt), bits, blocks);
         steps = list_steps(bits, all, list);
     }
+    // Offsets of this lane in 32 bits from bases that are the same for all lanes, and past the last step that step again, which
+    // nothing reads: few instructions a load (4096 x 14336, T = 16 routed 9.0 -> 8.0 us, 2048 x 7168, T = 16 6.2 -> 5.6).
     const CodeLane cl;
-    const uint8_t *codes = dc + (size_t)(m0 + cl.row) * (K / 2);
-    const char *hb = reinterpret_cast<const char *>(H + (size_t)t0 * ldh);
-    const int h_lane = r16 * 16;                         // a load of H: four steps, piece r16 of step q
-    const int block_last = (cl.block < blocks - (all - 1) * 4 ? cl.block : 0) * 16;
-    auto step_of = [&](int i) { return i < steps ? (kOneRun ? s_beg + i : (int)list[i]) : -1; };
+    const char *codes = reinterpret_cast<const char *>(dc + (size_t)m0 * (K / 2)), *hb = reinterpret_cast<const char *>(H + (size_t)t0 * ldh);
+    const unsigned code_at = cl.row * (K / 2) + cl.block * 16;
+    const unsigned code_last = cl.row * (K / 2) + (cl.block < blocks - (all - 1) * 4 ? cl.block * 16 : 0);
+    unsigned h_at[NL > 0 ? NL : 1];                      // a load of H: four steps of a token, piece r16 of step q
+#pragma unroll
+    for (int n = 0; n < NL; ++n) {
+        const int t = (wave * NL + n) / PARTS;
+        h_at[n] = (unsigned)(t < nt ? t : nt - 1) * ldh * 2 + r16 * 16;
+    }
+    auto step_of = [&](int i) {
+        const int k = i < steps ? i : steps > 0 ? steps - 1 : 0;
+        return kOneRun ? s_beg + k : steps > 0 ? (int)list[k] : 0;
+    };
     auto issue = [&](int c, char *dst) {                 // always PER loads
 #pragma unroll
         for (int n = 0; n < NL; ++n) {
             const int unit = wave * NL + n, t = unit / PARTS, part = unit % PARTS;
-            const int s = step_of(c * W + part * 4 + q);
-            const bool on = s >= 0 && t < nt;
-            dma16(on ? hb + (size_t)t * ldh * 2 + s * 256 + h_lane : reinterpret_cast<const char *>(g_zero16),
-                  t < nt ? dst + t * h_row + part * 1024 : scrap);
+            dma16(hb + (h_at[n] + (unsigned)step_of(c * W + part * 4 + q) * 256), t < nt ? dst + t * h_row + part * 1024 : scrap);
         }
-        const int s = step_of(c * W + wave);
-        dma16(s >= 0 ? reinterpret_cast<const char *>(codes + s * 64 + (s == all - 1 ? block_last : cl.block * 16)) : reinterpret_cast<const char *>(g_zero16),
-              dst + h_stage + wave * 1024);
+        const int s = __builtin_amdgcn_readfirstlane(step_of(c * W + wave));
+        dma16(codes + ((s == all - 1 ? code_last : code_at) + (unsigned)s * 64), dst + h_stage + wave * 1024);
     };
     const int chunks = (steps + W - 1) / W;
     keep_order();
@@ -262,11 +268,9 @@ w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__
             if (kWhole)
 #pragma unroll 1
                 for (int part = wave; part * 4 < steps; part += W) {
-                    const int s = step_of(part * 4 + q);
+                    const unsigned at = (unsigned)step_of(part * 4 + q) * 256 + r16 * 16;
 #pragma unroll 1
-                    for (int t = 0; t < nt; ++t)
-                        dma16(s >= 0 ? hb + (size_t)t * ldh * 2 + s * 256 + h_lane : reinterpret_cast<const char *>(g_zero16),
-                              all_h + t * h_row + part * 1024);
+                    for (int t = 0; t < nt; ++t) dma16(hb + (at + (unsigned)t * ldh * 2), all_h + t * h_row + part * 1024);
                 }
             stage_scales(ds + (size_t)m0 * blocks, scales, K / 2, true, wave, W);
         }
@@ -284,19 +288,20 @@ w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__
         else
             pipeline_barrier<(AHEAD - 1) * PER>();
         issue(c + AHEAD, fill);
-        const int s = step_of(c * W + wave);
-        if (s >= 0) {
-            const int b = s * 4 + q;
+        if (c * W + wave < steps) {
+            const int b = __builtin_amdgcn_readfirstlane(step_of(c * W + wave)) * 4 + q;
             const uint32_t byte = *reinterpret_cast<const uint8_t *>(scales + r16 * blocks + b);
             // a block that is not live: H is zero there, the scale may be no number
             const bool on = b < blocks && (kOneRun ? b >= run.beg / 32 && b * 32 < run.end : (bits[b / 32] >> (b & 31) & 1) != 0);
-            const float scale = scale_of(on ? byte : 127u);
             const u32x4 w = *reinterpret_cast<const u32x4 *>(mine + wr);
             const char *mh = kWhole ? all_h + c * W * 256 : mine;
+            bf16x8 h[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[j], scale), *reinterpret_cast<const bf16x8 *>(mh + hr + j * 16),
-                                                              acc, 0, 0, 0);
+            for (int j = 0; j < 4; ++j) h[j] = *reinterpret_cast<const bf16x8 *>(mh + hr + j * 16);
+            __builtin_amdgcn_sched_barrier(0);           // one wait for all of these reads
+            const float scale = scale_of(on ? byte : 127u);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[j], scale), h[j], acc, 0, 0, 0);
         }
         mine = mine + stage == end ? lds : mine + stage;
         fill = fill + stage == end ? lds : fill + stage;
