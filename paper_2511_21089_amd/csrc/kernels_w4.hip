@@ -59,7 +59,8 @@ size_t gate_up_lds(int nt, int nw, int S, int K, bool whole)
 // piece c lies at place c ^ r of its 256 bytes, and group q of lanes takes piece (block) 4 q + s in step s, so that the lanes of a
 // cycle read different banks; x lies in the order in which it is read.  The 16 rows' scales are staged whole: asking for a byte
 // a block costs as many requests as the codes (20.8 us).
-// 4096 x 14336: T = 1 15.2 us (62 MB, 4.1 TB/s), T = 16 17.5; 896 x 4864, T = 1 5.1, of which some 4.5 are the start, the first loads' latency and
+// 4096 x 14336: T = 1 13.7 us (62 MB, 4.5 TB/s), T = 16 16.3 (15.0 and 17.5 with a step's reads waited for one after the other and 64-bit
+// addresses); 896 x 4864, T = 1 4.3, of which some 4 are the start, the first loads' latency and
 // the epilogue's instruction fetch, which no kernel here is without.
 template <bool kOneRun, int XL, int S>
 __global__ void __launch_bounds__(512)
@@ -108,20 +109,35 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
         const int n0 = have ? groups(idx) * 8 : 0;
         if (at != (int)blockIdx.x) pipeline_barrier<0>();               // the last group's stages and scales have been read
         const char *xb = reinterpret_cast<const char *>(x + (size_t)t0 * K);
-        const uint8_t *gb = gc + (size_t)n0 * (K / 2), *ub = uc + (size_t)n0 * (K / 2);
+        // Offsets of this lane in 32 bits from bases that are the same for all lanes.  A wave without a group asks for zeros; in the last
+        // chunk what lies past the row's end is zero in x, and in the codes anything, the row's first.
+        const char *gb = have ? reinterpret_cast<const char *>(gc + (size_t)n0 * (K / 2)) : zero;
+        const char *ub = have ? reinterpret_cast<const char *>(uc + (size_t)n0 * (K / 2)) : zero;
+        unsigned x_at[XL > 0 ? XL : 1], code_at[4], code_last[4];
+#pragma unroll
+        for (int n = 0; n < XL; ++n) x_at[n] = (unsigned)(wave + n * nw < nt ? wave + n * nw : 0) * K * 2 + x_piece * 16;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int piece = r16 ^ (4 * r + q);         // of row 4 r + q
+            const unsigned row = (unsigned)(4 * (r & 1) + q) * (K / 2);
+            code_at[r] = have ? row + piece * 16 : 0;
+            code_last[r] = have ? row + ((chunks - 1) * 16 + piece < blocks ? (chunks - 1) * 16 + piece : 0) * 16 : 0;
+        }
         auto issue = [&](int i, char *dst) {             // always PER loads; past the end the last chunk again
             const int c = part + i * parts, k = c < chunks ? c : chunks - 1;
+            const bool last = k == chunks - 1;
+            const unsigned codes = have ? k * 256 : 0;
 #pragma unroll
             for (int n = 0; n < XL; ++n) {
-                const int t = wave + n * nw;
-                dma16(t < nt && k * 64 + x_piece < K / 8 ? xb + (size_t)t * K * 2 + k * 1024 + x_piece * 16 : zero, t < nt ? dst + t * kXRow : scrap);
+                const char *src = xb + (x_at[n] + k * 1024);
+                if (last && K % kChunkK != 0) {
+                    asm volatile("");                    // a branch: a select would take these instructions in every chunk
+                    src = k * 64 + x_piece < K / 8 ? src : zero;
+                }
+                dma16(src, wave + n * nw < nt ? dst + (wave + n * nw) * kXRow : scrap);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int piece = r16 ^ (4 * i + q);     // of row 4 i + q; past the row's end, where x is zero, its first
-                const int off = (4 * (i & 1) + q) * (K / 2) + (k * 16 + piece < blocks ? k * 16 + piece : 0) * 16;
-                dma16(have ? reinterpret_cast<const char *>((i < 2 ? gb : ub) + off) : zero, dst + cb + i * 1024);
-            }
+            for (int r = 0; r < 4; ++r) dma16((r < 2 ? gb : ub) + (last ? code_last[r] : code_at[r] + codes), dst + cb + r * 1024);
         };
         keep_order();
 #pragma unroll 1
@@ -152,16 +168,32 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
             issue(i + AHEAD, fill);
             const char *mx = kWhole ? all_x + c * nt * kXRow : mine;
             const char *sc = my_s + r16 * blocks + c * 16 + q * 4;
-            if (have)
+            if (have) {
+                // the next step's reads come after the first product: the compiler waits for all reads of LDS at the first use of one
+                uint32_t byte[2];
+                u32x4 w[2];
+                bf16x8 xv[2][4];
+                auto read = [&](int s) {
+                    byte[s & 1] = *reinterpret_cast<const uint8_t *>(sc + s);
+                    w[s & 1] = *reinterpret_cast<const u32x4 *>(mine + cb + r16 * 256 + ((q * 4 + s) ^ r16) * 16);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const uint32_t byte = *reinterpret_cast<const uint8_t *>(sc + s);
-                const float scale = scale_of(c * 16 + q * 4 + s < blocks ? byte : 127u);
-                const u32x4 w = *reinterpret_cast<const u32x4 *>(mine + cb + r16 * 256 + ((q * 4 + s) ^ r16) * 16);
+                    for (int j = 0; j < 4; ++j) xv[s & 1][j] = *reinterpret_cast<const bf16x8 *>(mx + xr + s * 256 + j * 16);
+                };
+                read(0);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        widen8(w[j], scale), *reinterpret_cast<const bf16x8 *>(mx + xr + s * 256 + j * 16), acc, 0, 0, 0);
+                for (int s = 0; s < 4; ++s) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    const float scale = scale_of(c * 16 + q * 4 + s < blocks ? byte[s & 1] : 127u);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[s & 1][j], scale), xv[s & 1][j], acc, 0, 0, 0);
+                        if (j == 0 && s < 3) {
+                            __builtin_amdgcn_sched_barrier(0);
+                            read(s + 1);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                }
             }
             mine = mine + stage == lds + S * stage ? lds : mine + stage;
             fill = fill + stage == lds + S * stage ? lds : fill + stage;
