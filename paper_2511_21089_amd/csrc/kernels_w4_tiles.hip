@@ -52,7 +52,7 @@ __device__ __forceinline__ void sum_steps(f32x4 (&acc)[NA][NF], const uint8_t *c
         x_k[i] = c * 8;
     }
     const CodeLane cl;
-    const int w_row = cl.row * (K / 2);
+    const unsigned w_row = cl.row * (K / 2);
     const int block_last = cl.block < blocks - (all - 1) * 4 ? cl.block : 0;     // in the last step there may be fewer than four
     const bool by16 = K % 512 == 0;
     const int late = by16 ? 0 : (r16 * blocks) & 3;                     // bytes of a dword before a row's
@@ -61,8 +61,8 @@ __device__ __forceinline__ void sum_steps(f32x4 (&acc)[NA][NF], const uint8_t *c
     int have = -1, slot = 0;                                            // the last 512 of K whose scales were asked for, and where
     auto issue = [&](int i, char *dst) {                                // stage i: steps KW i ..; always PER loads, and at times scales
         const int s = step_of(i * KW + kw);                             // past the end the last one again
-        if (s / 4 != have) {
-            have = s / 4;
+        if (s >> 2 != have) {
+            have = s >> 2;
             slot = slot == AHEAD ? 0 : slot + 1;
             char *to = my_s + slot * kScaleBuf;
             if (by16) {
@@ -81,7 +81,7 @@ __device__ __forceinline__ void sum_steps(f32x4 (&acc)[NA][NF], const uint8_t *c
             if (!kWholeSteps && u == all - 1) src = u * kStepK + x_k[j] < K ? src : zero;
             dma16(src, dst + (wave * NX + j) * 1024);
         }
-        const int off = w_row + s * 64 + (s == all - 1 ? block_last : cl.block) * 16;
+        const unsigned off = w_row + s * 64 + (s == all - 1 ? block_last : cl.block) * 16;
 #pragma unroll
         for (int a = 0; a < NA; ++a) dma16(codes[a] + off, dst + w_at + a * 1024);
     };
@@ -99,12 +99,13 @@ __device__ __forceinline__ void sum_steps(f32x4 (&acc)[NA][NF], const uint8_t *c
     for (int i = 0; i < stages; ++i) {
         pipeline_barrier<(AHEAD - 1) * PER>();
         const int s = step_of(i * KW + kw);
-        if (s / 4 != read) read = s / 4, rslot = rslot == AHEAD ? 0 : rslot + 1;
-        const int at = late + s % 4 * 4 + q;
+        if (s >> 2 != read) read = s >> 2, rslot = rslot == AHEAD ? 0 : rslot + 1;
+        const int at = late + (s & 3) * 4 + q;
         const char *sc = my_s + rslot * kScaleBuf + (by16 ? r16 * 16 + at : (at >> 2) * 256 + r16 * 4 + (at & 3));
         const char *st = mine + kw * (NF * 4096) + r16 * 256;
         const bool live = on(s * 4 + q), mine_too = KW == 1 || i * KW + kw < n;
         float scale[NA];
+        uint32_t byte[NA];
         u32x4 w[NA];
         bf16x8 xv[2][NF];
         auto read_x = [&](int j) {
@@ -113,13 +114,17 @@ __device__ __forceinline__ void sum_steps(f32x4 (&acc)[NA][NF], const uint8_t *c
         };
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-            const uint32_t byte = *reinterpret_cast<const uint8_t *>(sc + a * a_step);
+            byte[a] = *reinterpret_cast<const uint8_t *>(sc + a * a_step);
             w[a] = *reinterpret_cast<const u32x4 *>(mine + w_at + a * 1024 + cl.at);
-            // the second set has no step where their number is odd: codes of zero
-            if (KW > 1 && !mine_too) w[a] = u32x4{0, 0, 0, 0};
-            scale[a] = scale_of(live && mine_too ? byte : 127u);
         }
         read_x(0);
+        __builtin_amdgcn_sched_barrier(0);               // one wait for all of these reads
+#pragma unroll
+        for (int a = 0; a < NA; ++a) {
+            // the second set has no step where their number is odd: codes of zero
+            if (KW > 1 && !mine_too) w[a] = u32x4{0, 0, 0, 0};
+            scale[a] = scale_of(live && mine_too ? byte[a] : 127u);
+        }
         // The compiler waits for all reads of LDS at the first use of one, so the next reads come after the first products.
 #pragma unroll
         for (int j = 0; j < 4; ++j) {

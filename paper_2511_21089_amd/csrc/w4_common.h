@@ -221,6 +221,7 @@ __device__ __forceinline__ void clear_range(uint16_t *H, int ldh, int nt, int fr
             if (p >= from && p + 8 <= to)
                 *reinterpret_cast<u32x4 *>(h) = u32x4{0, 0, 0, 0};
             else
+#pragma unroll 1
                 for (int e = 0; e < 8; ++e)
                     if (p + e >= from && p + e < to) h[e] = 0;
         }
