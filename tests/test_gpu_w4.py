@@ -363,6 +363,27 @@ def test_graph(mm, T):
 
 
 # ------------------------------------------------------------------------------------------------ together
+@pytest.mark.parametrize("T", [2, 40])
+def test_two_streams_at_once(mm, T):
+    """Two layers on two streams, each with its workspace, again and again: what each gives alone."""
+    import torch
+    jobs = []
+    for seed in (1, 2):
+        x, packed, values, off, alpha = layer(mm, T, 512, [300, 212, 512], seed=seed)
+        ws = torch.empty(mm.mlpmoe_w4_workspace_bytes(T, 512, int(off[-1]), 3), dtype=torch.uint8, device="cuda")
+        args = (mm.bf16_tensor(x), *packed, off, alpha, np.ones(3, np.uint8))
+        jobs.append((args, ws, mm.mlpmoe_forward_w4(*args, workspace=ws), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for args, ws, _, stream in jobs:
+            with torch.cuda.stream(stream):
+                got.append(mm.mlpmoe_forward_w4(*args, workspace=ws))
+    torch.cuda.synchronize()
+    for i, out in enumerate(got):
+        assert torch.equal(out, jobs[i % 2][2])
+
+
 @pytest.mark.parametrize("T", [1, 16, 70])
 def test_router_and_forward_together(mm, T):
     """Logits -> route -> the forward on 4-bit weights, as a server runs them; the counts are those of the routes, and a
