@@ -52,7 +52,8 @@ size_t gate_up_lds(int nt, int nw, int S, int K, bool whole)
 
 // Grid (workgroups, tiles of tt tokens).  A wave works out groups of 8 neurons, MFMA rows 0-7 W_gate and 8-15 W_up; wave w of
 // workgroup g the groups w * grid + g and so on, so that what live groups there are is spread over the chip.  With x whole in
-// LDS (below) and waves left over, as where tokens take few branches, several waves share a group, chunk by chunk of K in turn.
+// LDS (below) several waves can share a group, chunk by chunk of K in turn: as many as the host says or, where the live groups are known
+// here only, as have none of their own (T = 1 on one of 8 or 16 branches, us with its events: 4096 x 14336 9.0, not shared 10.8, 8192 x 8192 10.1, 14.2).
 // 512 of K at a time, the codes (each wave its own) go through LDS, S - 1 stages ahead, and with them x (for the workgroup), which
 // has the waves meet for every stage; XL = 0: x fits LDS whole, and after one meeting every wave goes at its own pace.  A load of codes
 // is 256 bytes of four rows each: 4096 x 14336, gate and up codes alone, 10.2 us, and 11.3 us with 64 bytes of 16 rows.  Row r's 16-byte
@@ -88,7 +89,7 @@ w4_gate_up(const uint16_t *__restrict__ x, int T, int tt, int K, const uint8_t *
         clear_edges(off, bt.B, live, live, H + (size_t)t0 * ldh, ldh, nt, wave, nw, blockIdx.x, gridDim.x);
     }
 
-    // parts of K that a group's waves take in turn, and this wave's group and part
+    // this wave's group and part of K, of the parts that a group's waves take in turn
     int parts = kWhole && kOneRun ? parts_if_one : 1, slot = wave, part = 0;
     if constexpr (kWhole && !kOneRun) {
         const int own = __popcll(__ballot(lane < nw && (int)blockIdx.x + lane * (int)gridDim.x < groups.total));
@@ -456,10 +457,9 @@ hipError_t launch_gate_up(const W4Args &a, const BranchTable &bt, const Range &r
     return launch_status("w4_gate_up launch");
 }
 
-// A wave a group for every CU's share of the groups, up to 8; three stages, x whole if there is room for it.  Then waves can share
-// groups: in a routed call as many as there are to spare, the most being 8 (which groups are live, the kernel sees); in another
-// one from 8 chunks of K on.  us with their events, shared and not: T = 1 on one of 8 or 16 branches 4096 x 14336 12.8, 16.2, 8192 x 8192 11.8,
-// 19.9; T = 1 unrouted 6144 x 2048 8.8, 14.8, 4096 x 4096 10.0, 11.8, 8192 x 8192 20.3, 21.6, but 2048 x 7168 9.2, 8.9.  (More stages, that
+// A wave a group for every CU's share of the groups, up to 8; three stages, x whole if there is room for it.  Where the share is one or two
+// groups and K is long, 8 waves share them (T = 1, us with its events: 6144 x 2048 8.5, not shared 12.0, 4096 x 4096 9.6 and 10.0; but three or more:
+// 8192 x 8192 19.7 and 19.3, 2048 x 7168 8.9 and 8.0).  (More stages, that
 // is requests in flight, take longer: 4096 x 14336, T = 1: four 18.0 us, three 16.8.)  Where three stages with x in them do not fit,
 // up to two waves fewer, then two stages.  A wave loads up to four tokens of x.
 template <bool kOneRun>
@@ -469,8 +469,7 @@ hipError_t gate_up(const W4Args &a, const BranchTable &bt, const Range &run, int
     auto fits = [&](int nw, int S, bool whole) { return gate_up_lds(nt, nw, S, K, whole) <= (size_t)kLdsBytes; };
     int want = ceil_div(groups, 256);
     want = want > 8 ? 8 : want;
-    const int chunks = ceil_div(K, kChunkK);
-    const int nw = kOneRun ? (chunks < 8 ? want : want * (8 / want)) : chunks > 1 ? 8 : want;
+    const int nw = want <= 2 && K >= 8 * kChunkK ? 8 : want;
     if (fits(nw, 3, true)) return launch_gate_up<kOneRun, 0, 3>(a, bt, run, groups, want, nw, 16);
     if (fits(want, 3, true)) return launch_gate_up<kOneRun, 0, 3>(a, bt, run, groups, want, want, 16);
     want = want < least ? least : want;
@@ -486,15 +485,15 @@ hipError_t gate_up(const W4Args &a, const BranchTable &bt, const Range &run, int
     return launch_gate_up<kOneRun, 4, 2>(a, bt, run, groups, 1, 1, 4);      // scales of a very long K: one wave, four tokens at a time
 }
 
-// 16 waves while three stages of their chunks fit, else 8, whose chunks are half as long.  H whole if it fits for up to 8 tokens, us
-// against H by chunks: 4096 x 14336, T = 1 7.9, 8.7; 8192 x 8192, T = 1 12.2 and 13.5, T = 4 13.5 and 14.0; 2048 x 7168, T = 1 4.7 and 5.4,
-// T = 8 6.0 and 6.2, T = 12 7.0 and 6.4; 896 x 4864, T = 1 3.8 and 4.4.
+// 16 waves while three stages of their chunks fit, else 8, whose chunks are half as long.  H whole if it fits, us with its events against H by chunks:
+// 4096 x 14336, T = 1 9.6, 10.5; 8192 x 8192, T = 1 14.6 and 15.8, T = 4 15.4 and 16.0; 2048 x 7168, T = 1 6.8 and 7.2, T = 12 8.1 and 8.2;
+// 896 x 4864, T = 1 6.1 and 6.4.
 template <bool kOneRun>
 hipError_t down(const W4Args &a, const BranchTable &bt, const Range &run)
 {
     const int nt = a.T < 16 ? a.T : 16, K = a.d_inter;
     auto fits = [&](int W, int S, bool whole = false) { return down_lds(W, S, nt, K, kOneRun, whole) <= (size_t)kLdsBytes; };
-    if (nt <= 8 && fits(16, 4, true)) return launch_down<kOneRun, 16, 0, 4>(a, bt, run);
+    if (fits(16, 4, true)) return launch_down<kOneRun, 16, 0, 4>(a, bt, run);
     if (nt <= 4 && fits(16, 4)) return launch_down<kOneRun, 16, 1, 4>(a, bt, run);
     if (nt <= 8 && fits(16, 3)) return launch_down<kOneRun, 16, 2, 3>(a, bt, run);
     if (fits(8, 3)) return launch_down<kOneRun, 8, 4, 3>(a, bt, run);
