@@ -449,17 +449,18 @@ hipError_t launch_gate_up(const W4Args &a, const BranchTable &bt, const Range &r
     const hipError_t e = allow_lds<w4_gate_up<kOneRun, XL, S>>((int)lds, "w4_gate_up attribute");
     if (e != hipSuccess) return e;
     const int resident = 256 * (int)(160 * 1024 / lds);
-    const int grid = ceil_div(groups, share) < resident ? ceil_div(groups, share) : resident;
+    const int chunks = ceil_div(a.d_model, kChunkK), grid = ceil_div(groups, share) < resident ? ceil_div(groups, share) : resident;
     ProfileScope ps(MLPMOE_KERNEL_W4_GATE_UP, a.stream);
     w4_gate_up<kOneRun, XL, S><<<dim3(grid, ceil_div(a.T, tt)), nw * 64, lds, a.stream>>>(
         static_cast<const uint16_t *>(a.x), a.T, tt, a.d_model, a.gc, a.gs, a.uc, a.us, static_cast<uint16_t *>(a.H), a.ldh, a.route,
-        nw / share, run, bt);
+        nw / share < chunks ? nw / share : chunks, run, bt);
     return launch_status("w4_gate_up launch");
 }
 
-// A wave a group for every CU's share of the groups, up to 8; three stages, x whole if there is room for it.  Where the share is one or two
-// groups and K is long, 8 waves share them (T = 1, us with its events: 6144 x 2048 8.5, not shared 12.0, 4096 x 4096 9.6 and 10.0; but three or more:
-// 8192 x 8192 19.7 and 19.3, 2048 x 7168 8.9 and 8.0).  (More stages, that
+// A wave a group for every CU's share of the groups, up to 8; three stages, x whole if there is room for it.  Where the share is one to
+// three groups and a wave would have four or more kilobytes of x to load, up to 8 waves share them, or at least the loads (us with events,
+// shared and not: 4096 x 2048, T = 8 9.0, 16.2; 6144 x 2048, T = 1 8.4, 12.0; 2048 x 2048, T = 16 8.1, 14.7; 896 x 4864, T = 16 7.4, 7.7; but four groups: 2048 x 7168,
+// T = 4 8.9, 8.0).  (More stages, that
 // is requests in flight, take longer: 4096 x 14336, T = 1: four 18.0 us, three 16.8.)  Where three stages with x in them do not fit,
 // up to two waves fewer, then two stages.  A wave loads up to four tokens of x.
 template <bool kOneRun>
@@ -469,9 +470,9 @@ hipError_t gate_up(const W4Args &a, const BranchTable &bt, const Range &run, int
     auto fits = [&](int nw, int S, bool whole) { return gate_up_lds(nt, nw, S, K, whole) <= (size_t)kLdsBytes; };
     int want = ceil_div(groups, 256);
     want = want > 8 ? 8 : want;
-    const int nw = want <= 2 && K >= 8 * kChunkK ? 8 : want;
-    if (fits(nw, 3, true)) return launch_gate_up<kOneRun, 0, 3>(a, bt, run, groups, want, nw, 16);
-    if (fits(want, 3, true)) return launch_gate_up<kOneRun, 0, 3>(a, bt, run, groups, want, want, 16);
+    const int most = want <= 3 && ceil_div(K, kChunkK) * nt >= 4 * want ? 8 : want;
+    for (int n = most; n >= (want <= 2 && want < least ? least : want); --n)
+        if (fits(n, 3, true)) return launch_gate_up<kOneRun, 0, 3>(a, bt, run, groups, want, n, 16);
     want = want < least ? least : want;
     for (int n = want; n >= least && n >= want - 2; --n) {
         if (!fits(n, 3, false)) continue;

@@ -216,6 +216,19 @@ def test_routed_by_sequences(mm, T, run_length, d_model, widths):
 
 
 @pytest.mark.parametrize("kind", ["one run", "some off", "routed"])
+@pytest.mark.parametrize("T", [1, 5, 8, 13, 16])
+@pytest.mark.parametrize("d_model,widths", [(4096, [96, 32]), (2080, [500, 524, 1024]), (1024, [2000, 1000, 1096]), (6144, [1100, 948])])
+def test_waves_that_share(mm, T, d_model, widths, kind):
+    """Few neurons for many waves: K and the loads of x shared out, with and without a part left over."""
+    B = len(widths)
+    r = None
+    if kind == "routed":
+        r = np.zeros((T, B), np.uint8)
+        r[np.arange(T), np.arange(T) % 2] = 1
+    check(mm, T, d_model, widths, seed=T, off_branches=(1,) if kind == "some off" else (), route=r)
+
+
+@pytest.mark.parametrize("kind", ["one run", "some off", "routed"])
 @pytest.mark.parametrize("T,d_model,widths", [(300, 96, [256] * 8), (400, 96, [500, 512, 524, 512]), (600, 160, [256] * 8), (1100, 96, [2000, 48]),
                                               (1600, 2048, [1024, 1000, 1048, 1024])])
 def test_many_tokens(mm, T, d_model, widths, kind):
