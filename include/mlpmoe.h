@@ -362,8 +362,9 @@ MLPMOE_API int mlpmoe_forward_routed_f32_ws(const float *x, const float *W_gate,
  *   probs        device float [T, B], or NULL
  *   counts, loss device int32 [B + 1] and one float, or NULL, each for itself.  Without either the call is one launch and needs no
  *                workspace
- * An active logit that is not a number is never taken and makes its token's probabilities, and the loss, not a number; so does
- * plus infinity, which is taken first.  Arithmetic in float; sums over tokens in float within a block of tokens and in double
+ * An active logit that is not a number is never taken.  It does not bar its branch: its token counts, also if none of its logits is a
+ * number, and the loss and the token's probabilities, but for the barred branches, are not numbers; so it is with plus infinity, which is
+ * taken first.  Arithmetic in float; sums over tokens in float within a block of tokens and in double
  * over the blocks, in an order that follows from T and B: results are the same bits from run to run.  No output may overlap
  * an input.  T >= 0 (T == 0: counts and loss are set to zero), T <= 2^24, 1 <= B <= MLPMOE_MAX_BRANCHES.
  * Workspace as for mlpmoe_forward_bf16: mlpmoe_set_workspace()'s block or the library's own; the _ws form takes the caller's,

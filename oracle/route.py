@@ -1,7 +1,8 @@
 """The router of a routed layer in float64: which branches a token takes, probabilities, counts, balance loss and gradient.
 
 The loss is A * sum_b f_b P_b over the active branches: f_b the share of the assignments that go to branch b, P_b its mean
-probability over the tokens that count.  The counts have no gradient.
+probability over the tokens that count.  The counts have no gradient.  A logit of minus infinity bars its branch; one that is
+not a number is never taken, and its token counts, with probabilities that are not numbers.
 """
 import numpy as np
 
@@ -18,10 +19,10 @@ def route_topk(logits, k, active=None, real=None):
     for t in range(T):
         on = [b for b in range(B) if active[b] and not x[t, b] == -np.inf]
         numbers = [b for b in on if not np.isnan(x[t, b])]
-        if not real[t] or not numbers:
+        if not real[t] or not on:
             continue
         counts[B] += 1
-        top = max(x[t, b] for b in numbers)
+        top = max((x[t, b] for b in numbers), default=np.nan)
         with np.errstate(invalid="ignore"):
             e = {b: np.exp(x[t, b] - top) for b in on}
         s = sum(e.values())
@@ -31,7 +32,7 @@ def route_topk(logits, k, active=None, real=None):
             route[t, b] = 1
             counts[b] += 1
     taken = counts[:B].sum()
-    loss = 0.0
+    loss = float(np.sum(0.0 * probs))                # 0, or not a number
     if taken:
         loss = float(active.sum()) * float(np.sum(counts[:B] / taken * probs.sum(axis=0))) / counts[B]
     return route, probs, counts, loss
@@ -47,4 +48,4 @@ def route_backward(probs, counts, dprobs=None, dloss=0.0, n_active=None):
     if c[:B].sum() > 0:
         g = g + dloss * A * (c[:B] / c[:B].sum()) / c[B]
     g[p == 0] = 0.0
-    return p * (g - (p * g).sum(axis=1, keepdims=True))
+    return np.where(p == 0, 0.0, p * (g - (p * g).sum(axis=1, keepdims=True)))

@@ -47,6 +47,9 @@ struct Add {
 struct Max {
     __device__ __forceinline__ int operator()(int a, int b) const { return a > b ? a : b; }
 };
+struct Or {
+    __device__ __forceinline__ int operator()(int a, int b) const { return a | b; }
+};
 
 // Logits as integers in the same order, both zeros alike and what is not a number as -inf: the largest of two is one
 // instruction that takes its operand across lanes, where a float's needs two more to be quiet about not-a-numbers.
@@ -136,7 +139,8 @@ __device__ __forceinline__ void finish(double p, int c, int tokens, int B, int n
     if (counts && lane < B) counts[lane] = c;
     if (counts && lane == 0) counts[B] = tokens;
     const double sum = over_wave(p * (double)c), taken = over_wave((double)c);
-    if (loss && lane == 0) *loss = taken > 0 ? (float)((double)n_active * sum / (taken * (double)tokens)) : 0.0f;
+    // nothing taken: sum is 0, or not a number if a probability is none
+    if (loss && lane == 0) *loss = (float)(taken > 0 ? (double)n_active * sum / (taken * (double)tokens) : sum);
 }
 
 constexpr int kRouteThreads = 1024;
@@ -199,10 +203,17 @@ route_topk_kernel(const E *__restrict__ logits, int ld, unsigned long long activ
         }
         const int none = order(kNegInf);
         const int most = over_token<L>(s[0], more);
-        const bool used = most > none;
+        bool used = most > none;
 
         float p[4] = {0, 0, 0, 0};
         if (probs || kStats) {
+            // A token without a number to take is an empty row only if all of its branches are barred: with a not-a-number it counts,
+            // and m = -inf makes the probabilities of what is not barred not-a-numbers.  Looked at only where the wave has such a
+            // token: padding, mostly.
+            if (__ballot(!used) != 0) {
+                const bool nan = x[0] != x[0] || x[1] != x[1] || x[2] != x[2] || x[3] != x[3];
+                used = over_token<L>((int)(used || nan), Or()) != 0;
+            }
             const float m = value(most);
             float sum = 0;
 #pragma unroll
