@@ -427,8 +427,8 @@ MLPMOE_API int mlpmoe_w4_dequantize(const uint8_t *codes, const uint8_t *scales,
  * run.  An inactive branch, and one that no token takes, contributes nothing: no value of its weights reaches out, unless a block of
  * W_down that it shares with a neighbour has the scale 255.
  *
- * Workspace as for mlpmoe_forward_bf16; mlpmoe_w4_workspace_bytes() bytes (0 for invalid sizes; what serves T tokens serves fewer)
- * for the _ws form.
+ * Workspace as for mlpmoe_forward_bf16; mlpmoe_w4_workspace_bytes() bytes (0 for sizes that the forward refuses; what serves T
+ * tokens serves fewer) for the _ws form.
  * Errors: those of mlpmoe_forward_bf16, and UNSUPPORTED; T above 1048560 is MLPMOE_ERR_SHAPE.
  */
 MLPMOE_API size_t mlpmoe_w4_workspace_bytes(int T, int d_model, int d_inter, int B);

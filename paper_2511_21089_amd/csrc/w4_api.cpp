@@ -13,6 +13,14 @@ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 int w4_h_ld(int d_inter) { return (int)align_up((size_t)d_inter, 128); }
 size_t h_bytes(int T, int d_inter) { return align_up((size_t)T * w4_h_ld(d_inter) * 2, 256); }
 
+constexpr int kW4MaxTokens = 65535 * 16;
+
+// Rows that the kernels on 4-bit weights take: whole blocks, whose scales fit LDS.
+bool row_lengths_fit(int d_model, int d_inter)
+{
+    return d_model % 32 == 0 && d_inter % 32 == 0 && d_model <= kW4MaxK && d_inter <= kW4MaxK;
+}
+
 int check_matrix(const void *codes, const void *scales, const void *W, int rows, int cols, int elem_bytes)
 {
     if (rows < 0 || cols < 1 || rows > (1 << 22) || cols > (1 << 22) || (long long)rows * cols > (1LL << 40)) return MLPMOE_ERR_SHAPE;
@@ -29,12 +37,11 @@ int forward_w4(const void *x, const uint8_t *const w[6], const int32_t *off, con
 {
     int rc = check_forward(x, w[0], w[2], w[4], off, alpha, mask, T, d_model, d_inter, B, out);
     if (rc != MLPMOE_OK) return rc;
-    if ((out_bytes != 2 && out_bytes != 4) || d_model % 32 != 0 || d_inter % 32 != 0 || d_model > kW4MaxK || d_inter > kW4MaxK)
-        return MLPMOE_ERR_UNSUPPORTED;
+    if ((out_bytes != 2 && out_bytes != 4) || !row_lengths_fit(d_model, d_inter)) return MLPMOE_ERR_UNSUPPORTED;
     if (T == 0) return MLPMOE_OK;
     if (d_inter > 0 && (!w[1] || !w[3] || !w[5])) return MLPMOE_ERR_NULL;
     if (!aligned16(w[1]) || !aligned16(w[3]) || !aligned16(w[5])) return MLPMOE_ERR_ALIGN;
-    if (T > 65535 * 16) return MLPMOE_ERR_SHAPE;
+    if (T > kW4MaxTokens) return MLPMOE_ERR_SHAPE;
 
     (void)hipGetLastError();
     g_err_detail[0] = 0;
@@ -97,7 +104,8 @@ int mlpmoe_w4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, 
 
 size_t mlpmoe_w4_workspace_bytes(int T, int d_model, int d_inter, int B)
 {
-    if (T < 0 || d_model < 1 || d_inter < 0 || B < 1 || B > MLPMOE_MAX_BRANCHES) return 0;
+    if (T < 0 || T > kW4MaxTokens || d_model < 1 || d_inter < 0 || B < 1 || B > MLPMOE_MAX_BRANCHES) return 0;
+    if (!row_lengths_fit(d_model, d_inter)) return 0;
     return h_bytes(T, d_inter) + align_up(w4_partial_floats(T, d_model, d_inter) * 4, 256) + 256;
 }
 
