@@ -440,8 +440,16 @@ def _elem(dtype, what):
     raise ValueError("%s must be bfloat16 or float32" % what)
 
 
+# The library's sizes are 32-bit ints, and ctypes would pass the lower 32 bits of a larger one.
+_MOST = 0x7fffffff
+
+
+def _fit(*sizes):
+    return all(0 <= int(v) <= _MOST for v in sizes)
+
+
 def mlpmoe_route_workspace_bytes(T, B) -> int:
-    return int(lib.mlpmoe_route_workspace_bytes(int(T), int(B)))
+    return int(lib.mlpmoe_route_workspace_bytes(int(T), int(B))) if _fit(T, B) else 0
 
 
 def mlpmoe_route_topk(logits, k, active_mask=None, token_mask=None, route=None, probs=None, want_probs=True,
@@ -458,6 +466,9 @@ def mlpmoe_route_topk(logits, k, active_mask=None, token_mask=None, route=None, 
     if not logits.is_cuda or (logits.stride(1) != 1 and B > 1 and T > 0):
         raise ValueError("expected GPU logits whose rows are contiguous")
     ld = logits.stride(0) if T > 1 else B
+    k = int(k)
+    if not (T <= _MOST and B <= _MOST and ld <= _MOST and 0 <= k <= _MOST):
+        raise MlpMoeError(ERR_SHAPE, "mlpmoe_route_topk")
     if token_mask is not None and (tuple(token_mask.shape) != (T,) or token_mask.dtype not in (torch.uint8, torch.bool)):
         raise ValueError("token_mask must be a [T] uint8 or bool tensor")
     dev = logits.device
@@ -469,7 +480,7 @@ def mlpmoe_route_topk(logits, k, active_mask=None, token_mask=None, route=None, 
     ptrs = _here(token_mask, route, probs, counts, loss, workspace)
     if logits.get_device() != _current_device():
         raise ValueError("expected GPU tensors on the current device")
-    args = [logits.data_ptr(), ld, _bytes_mask(active_mask, B, "active_mask"), ptrs[0], T, B, int(k), elem, *ptrs[1:5]]
+    args = [logits.data_ptr(), ld, _bytes_mask(active_mask, B, "active_mask"), ptrs[0], T, B, k, elem, *ptrs[1:5]]
     if workspace is None:
         _check(lib.mlpmoe_route_topk(*args, _stream_ptr(stream)), "mlpmoe_route_topk")
     else:
@@ -491,6 +502,8 @@ def mlpmoe_route_backward(probs, counts, dprobs=None, dloss=None, active_mask=No
         raise ValueError("dloss must be a float32 tensor of one element")
     if counts is not None and (counts.dtype != torch.int32 or tuple(counts.shape) != (B + 1,)):
         raise ValueError("counts must be a [B + 1] int32 tensor")
+    if not (T <= _MOST and B <= _MOST):
+        raise MlpMoeError(ERR_SHAPE, "mlpmoe_route_backward")
     dlogits = _out(dlogits, (T, B), dtype, probs.device, "dlogits")
     p, c, dp, dl, out = _here(probs, counts, dprobs, dloss, dlogits)
     _check(lib.mlpmoe_route_backward(p, c, dp, dl, _bytes_mask(active_mask, B, "active_mask"), T, B, elem, out,
@@ -504,6 +517,8 @@ def mlpmoe_w4_quantize(W, codes=None, scales=None, stream=None):
     [rows, cols / 32]), both uint8."""
     rows, cols = W.shape
     elem = _elem(W.dtype, "W")
+    if not (rows <= _MOST and cols <= _MOST):
+        raise MlpMoeError(ERR_SHAPE, "mlpmoe_w4_quantize")
     codes = _out(codes, (rows, cols // 2), torch.uint8, W.device, "codes")
     scales = _out(scales, (rows, cols // 32), torch.uint8, W.device, "scales")
     w, c, s = _here(W, codes, scales)
@@ -529,6 +544,8 @@ def mlpmoe_w4_dequantize(codes, scales, dtype=None, out=None, stream=None):
     if dtype is None:
         dtype = torch.bfloat16 if out is None else out.dtype
     elem = _elem(dtype, "out")
+    if not (rows <= _MOST and cols <= _MOST):
+        raise MlpMoeError(ERR_SHAPE, "mlpmoe_w4_dequantize")
     out = _out(out, (rows, cols), dtype, codes.device, "out")
     c, s, w = _here(codes, scales, out)
     _check(lib.mlpmoe_w4_dequantize(c, s, rows, cols, elem, w, _stream_ptr(stream)), "mlpmoe_w4_dequantize")
@@ -536,6 +553,8 @@ def mlpmoe_w4_dequantize(codes, scales, dtype=None, out=None, stream=None):
 
 
 def mlpmoe_w4_workspace_bytes(T, d_model, d_inter, B) -> int:
+    if not _fit(T, d_model, d_inter, B):
+        return 0
     return int(lib.mlpmoe_w4_workspace_bytes(int(T), int(d_model), int(d_inter), int(B)))
 
 
@@ -549,6 +568,8 @@ def mlpmoe_forward_w4(x, gate, up, down, branch_offsets, alpha, active_mask, rou
     d_inter = int(off[-1])
     if x.dtype != torch.bfloat16:
         raise ValueError("x must be bfloat16")
+    if not (T <= _MOST and d_model <= _MOST):
+        raise MlpMoeError(ERR_SHAPE, "mlpmoe_forward_w4")
     if not (_w4_fits(*gate, d_inter, d_model) and _w4_fits(*up, d_inter, d_model) and _w4_fits(*down, d_model, d_inter)):
         raise ValueError("4-bit weights are codes [rows, cols / 2] and scales [rows, cols / 32], both uint8, and these do not fit x "
                          "and branch_offsets")
