@@ -39,7 +39,6 @@ struct BranchTable {
 struct BranchLanes {
     int v_next;
     float v_alpha;
-    BranchLanes() = default;
     __device__ __forceinline__ explicit BranchLanes(const BranchTable &bt)
     {
         const int lane = threadIdx.x & 63;
