@@ -454,8 +454,10 @@ def mlpmoe_route_workspace_bytes(T, B) -> int:
 
 def mlpmoe_route_topk(logits, k, active_mask=None, token_mask=None, route=None, probs=None, want_probs=True,
                       want_stats=True, workspace=None, stream=None):
-    """The k branches each token takes, from the router's logits [T, B] (bf16 or float32, rows of any stride).
+    """The k branches each token takes, from the router's logits [T, B] (bf16 or float32, rows of any stride below 2^31).
 
+    Like every call here it is no node of autograd's graph, whatever logits.requires_grad says: mlpmoe_route_backward gives the
+    gradient of the logits, for the caller's own backward pass.
     active_mask: host, B entries; token_mask: GPU, T bytes (uint8 or bool), 0 = padding.  Returns (route [T, B] uint8,
     probs [T, B] float32 or None, counts [B + 1] int32 or None, loss [1] float32 or None): counts[B] is the number of
     tokens counted, loss the balance loss."""
@@ -491,7 +493,8 @@ def mlpmoe_route_topk(logits, k, active_mask=None, token_mask=None, route=None, 
 
 def mlpmoe_route_backward(probs, counts, dprobs=None, dloss=None, active_mask=None, dtype=None, dlogits=None, stream=None):
     """Gradient of the router's logits from those of probs ([T, B] float32) and of the loss ([1] float32), either of
-    which may be None; in dtype (bfloat16 or float32, float32 if neither it nor dlogits is given)."""
+    which may be None; in dtype (bfloat16 or float32, float32 if neither it nor dlogits is given).  active_mask as given to
+    mlpmoe_route_topk."""
     T, B = probs.shape
     if dtype is None:
         dtype = torch.float32 if dlogits is None else dlogits.dtype

@@ -147,7 +147,7 @@ constexpr int kRouteThreads = 1024;
 
 // A token on L lanes, four branches a lane; a wave's next tokens are asked for before these are worked on.  Bound by vector
 // instructions, some 140 for four tokens of 64 branches and 11 a round of the selection: 131072 x 64 floats, k = 8, with
-// probabilities and sums 20.7 us, 3.6 TB/s (30.6 with float maxima, each three instructions a step instead of one, and the last
+// probabilities and sums 20.8 us, 3.6 TB/s, some 12 of them instructions and the rest the rounds' chain, each waiting for the one before (30.6 with float maxima, each three instructions a step instead of one, and the last
 // token's byte waited for before anything else); twice the blocks 20.0, and 5.5 us instead of 3.8 for the kernel after it.
 // kStats: also what the counts and the loss need: with one block the result, else the block's partial sums, rows of B and the
 // number of tokens.

@@ -60,8 +60,8 @@ size_t gate_up_lds(int nt, int nw, int S, int K, bool whole)
 // piece c lies at place c ^ r of its 256 bytes, and group q of lanes takes piece (block) 4 q + s in step s, so that the lanes of a
 // cycle read different banks; x lies in the order in which it is read.  The 16 rows' scales are staged whole: asking for a byte
 // a block costs as many requests as the codes (20.8 us).
-// 4096 x 14336: T = 1 13.7 us (62 MB, 4.5 TB/s), T = 16 16.3 (15.0 and 17.5 with a step's reads waited for one after the other and 64-bit
-// addresses); 896 x 4864, T = 1 4.3, of which some 4 are the start, the first loads' latency and
+// Medians of a trace, 4096 x 14336: T = 1 14.4 to 15.0 us (62 MB, 4.2 TB/s), T = 16 17.0, on a part of the branches 13.9 (16.3, 18.0 and 15.6 with
+// a step's reads waited for one after the other and 64-bit addresses); 896 x 4864, T = 1 4.6, of which some 4 are the start, the first loads' latency and
 // the epilogue's instruction fetch, which no kernel here is without.
 template <bool kOneRun, int XL, int S>
 __global__ void __launch_bounds__(512)
@@ -236,7 +236,7 @@ size_t down_lds(int W, int S, int nt, int K, bool one, bool whole)
 // steps of K each wave has one, so that together the waves read W * 64 bytes of a row.  Codes (each wave its own) and H (for the
 // workgroup) go through LDS, S - 1 chunks ahead, and the waves meet for every chunk; NL = 0: H of up to 16 tokens lies in LDS whole, and
 // after one meeting every wave goes at its own pace.  A step is live if a live branch has a neuron in it; the others are left out.  The waves' sums are added in
-// their order.  4096 x 14336: T = 1 7.5 us (31 MB, 4.1 TB/s), T = 16 12.3, bound by H, which every workgroup reads (117 MB out of L2;
+// their order.  Medians of a trace, 4096 x 14336: T = 1 7.6 us (31 MB, 4.1 TB/s), T = 16 12.3, bound by H, which every workgroup reads (117 MB out of L2;
 // four waves more that only load H, so that codes can be asked for five chunks ahead, do not help).
 // Asking for the codes at the end of the kernel before does not help: with all of them in L2 this one takes 7.6 us instead
 // of 8.4 (H by chunks), and that one longer by more.
@@ -268,7 +268,8 @@ w4_down(const uint16_t *__restrict__ H, int ldh, int T, int K, const uint8_t *__
         steps = list_steps(bits, all, list);
     }
     // Offsets of this lane in 32 bits from bases that are the same for all lanes, and past the last step that step again, which
-    // nothing reads: few instructions a load (4096 x 14336, T = 16 routed 9.0 -> 8.0 us, 2048 x 7168, T = 16 6.2 -> 5.6).
+    // nothing reads: few instructions a load (medians of a trace, T = 16: 4096 x 14336 on a part of the branches 11.2 -> 10.2 us, on all 12.5 -> 12.4,
+    // 2048 x 7168 6.5 -> 6.3).
     const CodeLane cl;
     const char *codes = reinterpret_cast<const char *>(dc + (size_t)m0 * (K / 2)), *hb = reinterpret_cast<const char *>(H + (size_t)t0 * ldh);
     const unsigned code_at = cl.row * (K / 2) + cl.block * 16;

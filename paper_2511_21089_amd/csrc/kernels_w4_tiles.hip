@@ -10,9 +10,9 @@
 // Rows are the MFMA's rows and tokens its columns: a lane ends with four neighbouring neurons (features) of a token, one store.
 // Nothing is loaded into registers: beside loads into LDS the compiler waits for every register load at once.
 //
-// 4096 x 14336, T = 500: gate and up 107 us (1.10 PFLOP/s), down 63 and the sum of its ranges 6.5.  Matrix pipes busy 47 % of it, LDS 40 %;
+// 4096 x 14336, T = 500: gate and up 106 us (1.11 PFLOP/s), down 63 and the sum of its ranges 6.6.  Matrix pipes busy 47 % of it, LDS 40 %;
 // without any loads the same loops take 95 us instead of 112 and 51 instead of 66 (with their events); the rest is the meetings
-// and the first reads of a stage.  T = 45: 23 and 16 us, start and latency again.
+// and the first reads of a stage.  T = 45: 24, 15 and 4 us, start and latency again.
 #include "w4_common.h"
 
 namespace mlpmoe {
